@@ -46,7 +46,8 @@ typedef enum {
     SB_ERR_UNSUPPORTED = -3, /* d is not 32, 64 or 128 */
     SB_ERR_ALIGN = -4,       /* a pointer is not 16-byte aligned */
     SB_ERR_LAUNCH = -5,      /* the HIP launch reported an error */
-    SB_ERR_WORKSPACE = -6    /* workspace missing or too small */
+    SB_ERR_WORKSPACE = -6,   /* workspace missing or too small */
+    SB_ERR_OVERLAP = -7      /* an output overlaps an input that is still read */
 } sb_status;
 
 /*
@@ -235,6 +236,75 @@ int sb_attn_decode(const void* q, const void* k, const void* v, const void* r, v
 #define SB_DECODE_STATIC_BYTES ((size_t)33554432)
 int sb_attn_decode_static(const void* q, const void* k, const void* v, const void* r, void* o, float* m,
                           int B, int H, int Hkv, int T, int Tcap, int d, void* stream);
+
+/*
+ * A key/value cache in 4 bits.  32 consecutive columns of a row share a power of two, held as a
+ * byte E that stands for 2^(E-127); a value is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it (codes 0
+ * to 7, the sign in bit 3), two codes to a byte, the even column in the low half.  (These are the
+ * public MX formats E2M1 and E8M0.)  kc, vc: codes, [B, Hkv, Tcap, d/2] bytes; ks, vs: scales,
+ * [B, Hkv, Tcap, d/32] bytes; Tcap a multiple of 32 (SB_ERR_SHAPE otherwise), at most 2^26;
+ * B*Hkv <= 65535.  A row takes d/2 + d/32 bytes (68 at d = 128; bf16: 256).
+ *   sb_attn_kv4_store  rows k, v [B, Hkv, n, d] bf16 into rows pos[b] .. pos[b]+n-1 of entry b
+ *                      (pos: B ints on the DEVICE, or NULL: 0); 1 <= n <= Tcap.  Rows that would
+ *                      lie outside 0 .. Tcap-1 are left out.  The scale of a block is the smallest
+ *                      power of two, 2^-120 at least, of which no magnitude is more than 7 times;
+ *                      values are rounded to the nearest, ties to the even code, beyond 6 to 6.  A
+ *                      block that holds a NaN or an infinity gets E = 255 and is NaN throughout.
+ *   sb_attn_kv4_load   the values of those rows as bf16 [B, Hkv, n, d], exactly; zeros for rows
+ *                      outside the cache.
+ */
+int sb_attn_kv4_store(const void* k, const void* v, void* kc, void* ks, void* vc, void* vs, const int* pos,
+                      int B, int Hkv, int n, int Tcap, int d, void* stream);
+int sb_attn_kv4_load(const void* kc, const void* ks, const void* vc, const void* vs, void* k, void* v, const int* pos,
+                     int B, int Hkv, int n, int Tcap, int d, void* stream);
+
+/*
+ * sb_attn_decode on a 4-bit cache: the same attention, of the values that the cache stands for.
+ * lens: B ints on the DEVICE, the rows of every entry (0 .. T; larger ones count as T, negative
+ * ones as 0), or NULL: T each.  1 <= T <= Tcap bounds them and sizes the launch.  Where an entry is
+ * empty, o is 0 (r with the bias) and m is 0.  Rows behind an entry's last are not looked at.
+ * score_out: optional fp32 [B, Hkv, Tcap].  score_out[b,h,i] = score[b,h,i] + sum over the query
+ * heads of kv head h of A[i], for the entry's rows i; others are left as they were.  score may be
+ * NULL (zeros) and may be score_out itself.  At most 1024 query heads a kv head with score_out.
+ * The weights that meet V are rounded to 16 bits (o itself has 8); score gets them in fp32.
+ * workspace: sb_attn_decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, score_out != NULL) bytes.
+ * Bit-reproducible, as sb_attn_decode.
+ */
+size_t sb_attn_decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d, int scores);
+int sb_attn_decode_kv4(const void* q, const void* kc, const void* ks, const void* vc, const void* vs, const void* r, const int* lens,
+                       const float* score, float* score_out, void* o, float* m, void* workspace, size_t workspace_bytes,
+                       int B, int H, int Hkv, int T, int Tcap, int d, void* stream);
+
+/*
+ * The weight that a prompt's queries give each key: score_out[b,h,i] = score[b,h,i] + sum over query
+ * rows j and the query heads of kv head h of A[i,j] (Eq. 1), for the entry's rows i; others are left
+ * as they were.  score may be NULL (zeros) and may be score_out itself.
+ * q: bf16 [B, H, Tq, d]; k: bf16 [B, Hkv, Tcap, d].  lens, qlens: B ints each on the DEVICE, the rows
+ * and the query rows of every entry, or NULL: T, Tq (clamped to 0 .. T and 0 .. Tq; what lies behind
+ * them is not looked at).  The queries are those of the entry's last rows: query row t < qlens[b]
+ * stands at row lens[b] - qlens[b] + t and weighs the keys before it.  Tq = T: the whole prompt;
+ * Tq = 1, its key appended already: one token.  1 <= Tq <= T <= Tcap, T <= 524288, B*Hkv <= 65535.
+ * workspace: sb_attn_key_weight_workspace_bytes(B, H, Hkv, Tq, T, d) bytes: 4*(T+63) for each 128 query
+ * rows of each group.  Bit-reproducible.
+ */
+size_t sb_attn_key_weight_workspace_bytes(int B, int H, int Hkv, int Tq, int T, int d);
+int sb_attn_key_weight(const void* q, const void* k, const int* lens, const int* qlens, const float* score, float* score_out,
+                       void* workspace, size_t workspace_bytes, int B, int H, int Hkv, int Tq, int T, int Tcap, int d, void* stream);
+
+/*
+ * Eviction by accumulated weight.  Of every (entry, kv head) the `recent` newest rows stay and, of the
+ * others, those with the highest scores: `keep` rows in all, or every row where an entry has no more.
+ * Equal scores: the lowest row first; NaN counts as above everything.  Rows keep their order (all that
+ * stick-breaking attention knows of positions), so what is left is a cache as any other.
+ * score: fp32 [B, Hkv, Tcap]; lens: as above.  The rows of `arrays` (0 .. 8) arrays move with their
+ * scores: src[i] [B, Hkv, Tcap, row_bytes[i]] to the first rows of dst[i] [B, Hkv, Tcap_out, row_bytes[i]],
+ * score to score_out [B, Hkv, Tcap_out]; what lies behind them is left as it was.  src, dst and
+ * row_bytes (1 .. 65536) are HOST arrays, read before the call returns.  index [B, Hkv, keep]: the rows that
+ * stayed, ascending, then -1.  lens_out [B]: the rows left, min(lens[b], keep).
+ * 1 <= keep <= Tcap_out, 0 <= recent <= keep.  No output may overlap an input (SB_ERR_OVERLAP).
+ */
+int sb_attn_evict(const float* score, const int* lens, const void* const* src, void* const* dst, const int* row_bytes, int arrays,
+                  float* score_out, int* index, int* lens_out, int B, int Hkv, int T, int Tcap, int Tcap_out, int keep, int recent, void* stream);
 
 /* Human-readable name of a status code (static storage). */
 const char* sb_status_string(int status);

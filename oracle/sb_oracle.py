@@ -214,3 +214,69 @@ def decode(q, k, v, r=None):
     o, rem = fwd_gqa(qf, np.concatenate([k, pad], axis=2), np.concatenate([v, pad], axis=2),
                      rows=(T, T + 1), r=r)
     return o[:, :, 0], rem[:, :, 0]
+
+
+def row_weights(q, k):
+    """One query row q [d] against keys k [T,d], all visible: (A [T], what is left of the stick), by Eq. 1's product."""
+    q, k = np.asarray(q, dtype=np.float64), np.asarray(k, dtype=np.float64)
+    z = k @ q / np.sqrt(k.shape[1])
+    e = np.exp(-np.abs(z))
+    take, leave = np.where(z >= 0, 1.0, e) / (1.0 + e), np.where(z >= 0, e, 1.0) / (1.0 + e)      # sigma(z), 1 - sigma(z)
+    behind = np.concatenate([np.cumprod(leave[::-1])[::-1][1:], np.ones(min(1, len(z)))])
+    return take * behind, float(np.prod(leave))
+
+
+KV4_GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def kv4(x):
+    """Rows x [..,d] (finite) in 4 bits: (codes [..,d], scale bytes [..,d/32]).  The scale is the smallest power of two, 2^-120 at
+    least, of which no magnitude of the 32 is more than 7 times; nearest value, ties to the even code."""
+    x = np.asarray(x, dtype=np.float64)
+    x = x.reshape(x.shape[:-1] + (-1, 32))
+    top = np.abs(x).max(-1)
+    byte = np.full(top.shape, 7, dtype=np.int64)
+    for E in range(8, 255):
+        byte = np.where(top > 7.0 * 2.0 ** (E - 1 - 127), E, byte)
+    y = np.abs(x) / 2.0 ** (byte[..., None] - 127.0)
+    far = np.abs(y[..., None] - KV4_GRID)
+    best = far.min(-1, keepdims=True)
+    near = far == best                                   # one or two neighbours: of two the even one
+    first = near.argmax(-1)
+    code = np.where((near.sum(-1) == 2) & (first % 2 == 1), first + 1, first)
+    code = code + 8 * np.signbit(x)
+    return code.reshape(code.shape[:-2] + (-1,)), byte
+
+
+def kv4_values(codes, scales):
+    """What codes [..,d] and scale bytes [..,d/32] stand for; NaN where the byte is 255."""
+    codes, scales = np.asarray(codes), np.asarray(scales, dtype=np.float64)
+    unit = np.where(scales == 255, np.nan, 2.0 ** (scales - 127.0))
+    return np.repeat(unit, 32, axis=-1) * KV4_GRID[codes & 7] * np.where(codes & 8, -1.0, 1.0)
+
+
+def key_weight(q, k, lens=None, qlens=None):
+    """q [B,H,Tq,d], the queries of the last rows of their entries, k [B,Hkv,T,d]: the sum over queries and the heads of a
+    group of the weight that each key gets, [B,Hkv,T]."""
+    q, k = np.asarray(q, dtype=np.float64), np.asarray(k, dtype=np.float64)
+    B, H, Tq, _ = q.shape
+    Hkv, T = k.shape[1], k.shape[2]
+    out = np.zeros((B, Hkv, T))
+    for b in range(B):
+        n, nq = (T if lens is None else int(lens[b])), (Tq if qlens is None else int(qlens[b]))
+        for h in range(H):
+            g = h // (H // Hkv)
+            for t in range(nq):
+                at = n - nq + t
+                if at > 0:
+                    out[b, g, :at] += row_weights(q[b, h, t], k[b, g, :at])[0]
+    return out
+
+
+def evict(score, n, keep, recent):
+    """The rows, ascending, that stay of the n rows of one head: the `recent` newest, and the highest scores of the others."""
+    if n <= keep:
+        return list(range(n))
+    older = max(0, n - recent)
+    best = sorted(range(older), key=lambda i: (-float(score[i]), i))[:keep - (n - older)]
+    return sorted(best) + list(range(older, n))

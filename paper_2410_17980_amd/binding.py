@@ -27,6 +27,8 @@ EXPORTS = (
     "sb_attn_fwd_rb", "sb_attn_bwd_rb", "sb_attn_fwd_gqa", "sb_attn_bwd_gqa",
     "sb_attn_varlen_fwd", "sb_attn_varlen_bwd_workspace_bytes", "sb_attn_varlen_bwd_gqa_workspace_bytes", "sb_attn_varlen_bwd",
     "sb_attn_decode_workspace_bytes", "sb_attn_decode", "sb_attn_decode_static",
+    "sb_attn_kv4_store", "sb_attn_kv4_load", "sb_attn_decode_kv4_workspace_bytes", "sb_attn_decode_kv4",
+    "sb_attn_key_weight_workspace_bytes", "sb_attn_key_weight", "sb_attn_evict",
     "sb_diag_mfma_rate", "sb_diag_stream_read", "sb_diag_fwd_clock", "sb_diag_fwd_tri",
     "sb_status_string", "sb_version",
 )
@@ -94,6 +96,20 @@ def load(build_if_missing: bool = True):
     lib.sb_attn_decode.restype = ci
     lib.sb_attn_decode_static.argtypes = [vp, vp, vp, vp, vp, fp, ci, ci, ci, ci, ci, ci, vp]
     lib.sb_attn_decode_static.restype = ci
+    lib.sb_attn_kv4_store.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, vp]
+    lib.sb_attn_kv4_store.restype = ci
+    lib.sb_attn_kv4_load.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, vp]
+    lib.sb_attn_kv4_load.restype = ci
+    lib.sb_attn_decode_kv4_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci, ci]
+    lib.sb_attn_decode_kv4_workspace_bytes.restype = ctypes.c_size_t
+    lib.sb_attn_decode_kv4.argtypes = [vp, vp, vp, vp, vp, vp, vp, fp, fp, vp, fp, vp, ctypes.c_size_t, ci, ci, ci, ci, ci, ci, vp]
+    lib.sb_attn_decode_kv4.restype = ci
+    lib.sb_attn_key_weight_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
+    lib.sb_attn_key_weight_workspace_bytes.restype = ctypes.c_size_t
+    lib.sb_attn_key_weight.argtypes = [vp, vp, vp, vp, fp, fp, vp, ctypes.c_size_t, ci, ci, ci, ci, ci, ci, ci, vp]
+    lib.sb_attn_key_weight.restype = ci
+    lib.sb_attn_evict.argtypes = [fp, vp, vp, vp, vp, ci, fp, vp, vp, ci, ci, ci, ci, ci, ci, ci, vp]
+    lib.sb_attn_evict.restype = ci
     lib.sb_diag_mfma_rate.argtypes = [vp, ctypes.c_size_t, ci, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.sb_diag_mfma_rate.restype = ci
     lib.sb_diag_stream_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
@@ -265,6 +281,51 @@ def sb_attn_decode_static(q, k, v, o, T=None, r=None, m=None, stream=None):
     """sb_attn_decode on the library's own static device scratch: nothing is allocated, so the
     caller passes every output (o [B,H,d] bf16, optionally m [B,H] fp32)."""
     return (_ext or _load_ext()).decode(q, k, v, T, r, o, m, False, None, stream, True)
+
+
+def sb_attn_kv4_store(k, v, kc, ks, vc, vs, pos=None, stream=None):
+    """Rows k, v [B,Hkv,n,d] (bf16) into a 4-bit cache: codes kc, vc [B,Hkv,Tcap,d/2] and scales ks, vs
+    [B,Hkv,Tcap,d/32], all uint8, Tcap a multiple of 32; into rows pos[b] .. pos[b] + n - 1 (int32 [B] on
+    the GPU; 0 when not given).  Rows outside the cache are left out."""
+    (_ext or _load_ext()).kv4_store(k, v, kc, ks, vc, vs, pos, stream)
+
+
+def sb_attn_kv4_load(kc, ks, vc, vs, n, pos=None, k=None, v=None, stream=None):
+    """The values of n rows of a 4-bit cache from pos[b] on (0 when not given).  Returns (k, v), bf16 [B,Hkv,n,d]."""
+    return (_ext or _load_ext()).kv4_load(kc, ks, vc, vs, n, pos, k, v, stream)
+
+
+def sb_attn_decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, scores=False) -> int:
+    return int(load().sb_attn_decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, int(scores)))
+
+
+def sb_attn_decode_kv4(q, kc, ks, vc, vs, T=None, lens=None, r=None, score=None, score_out=None, o=None, m=None, want_m=False,
+                       workspace=None, stream=None):
+    """Single-token decode on a 4-bit cache: q [B,H,d] against the first lens[b] rows of entry b (int32 [B] on the
+    GPU, at most T; T, which defaults to Tcap, when not given).  score_out [B,Hkv,Tcap] fp32 (score itself where only that
+    is given) = score + the weight that the token gives each of those rows; score alone may be left out (zeros).
+    Returns o [B,H,d] (bf16), or a tuple of it and, as far as they are wanted, m and score_out."""
+    return (_ext or _load_ext()).decode_kv4(q, kc, ks, vc, vs, T, lens, r, score, score_out, o, m, want_m, workspace, stream)
+
+
+def sb_attn_key_weight_workspace_bytes(B, H, Hkv, Tq, T, d) -> int:
+    return int(load().sb_attn_key_weight_workspace_bytes(B, H, Hkv, Tq, T, d))
+
+
+def sb_attn_key_weight(q, k, T=None, lens=None, qlens=None, score=None, score_out=None, workspace=None, stream=None):
+    """The weight that the queries q [B,H,Tq,d] of an entry's last rows give its keys, the first lens[b] rows of
+    k [B,Hkv,Tcap,d] (at most T, which defaults to Tcap); qlens[b] of the query rows count.  Returns score_out [B,Hkv,Tcap]
+    fp32 = score (zeros when not given) + that weight; score is updated in place where only that is given."""
+    return (_ext or _load_ext()).key_weight(q, k, T, lens, qlens, score, score_out, workspace, stream)
+
+
+def sb_attn_evict(score, rows, keep, recent=0, T=None, lens=None, out=None, score_out=None, lens_out=None, index=None, stream=None):
+    """Keeps `keep` rows of every (entry, kv head): the `recent` newest and the highest scores [B,Hkv,Tcap] among the others.
+    rows: the tensors [B,Hkv,Tcap,...] that move (k, v, or the four of a 4-bit cache), out: where to [B,Hkv,Tcap_out,...], none
+    of them an input.  Returns (out, score_out, lens_out, index): out a tuple of tensors as large as rows where none were
+    given, score_out [B,Hkv,Tcap_out], lens_out int32 [B], index int32 [B,Hkv,keep] (the rows that stayed, then -1)."""
+    return (_ext or _load_ext()).evict(score, tuple(rows), keep, recent, T, lens, None if out is None else tuple(out), score_out, lens_out, index,
+                                       stream)
 
 
 def sb_attn_bwd_dq(q, k, v, m, dout, dq=None, workspace=None, stream=None):

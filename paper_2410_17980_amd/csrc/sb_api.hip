@@ -290,6 +290,155 @@ int sb_attn_decode_static(const void* q, const void* k, const void* v, const voi
     return e == hipSuccess ? SB_OK : SB_ERR_LAUNCH;
 }
 
+namespace {
+// rows of a cache: counted with 32 bits, and a launch takes fewer than 2^32 threads along its rows
+constexpr int MOST_ROWS = 1 << 26;
+
+int check_cache(int B, int Hkv, int Tcap, int d)
+{
+    if (B < 1 || Hkv < 1 || Tcap < 1 || Tcap > MOST_ROWS || (double)B * Hkv > 65535.0) return SB_ERR_SHAPE;
+    if (d != 32 && d != 64 && d != 128) return SB_ERR_UNSUPPORTED;
+    if ((double)B * Hkv * Tcap * d >= 1099511627776.0) return SB_ERR_SHAPE;
+    return SB_OK;
+}
+
+int check_kv4(int B, int Hkv, int Tcap, int d)
+{
+    if (int rc = check_cache(B, Hkv, Tcap, d)) return rc;
+    return Tcap % 32 ? SB_ERR_SHAPE : SB_OK;
+}
+
+int check_kv4_rows(const void* kc, const void* ks, const void* vc, const void* vs, const void* k, const void* v, const int* pos,
+                   int B, int Hkv, int n, int Tcap, int d)
+{
+    if (!kc || !ks || !vc || !vs || !k || !v) return SB_ERR_NULL;
+    if (int rc = check_kv4(B, Hkv, Tcap, d)) return rc;
+    if (n < 1 || n > Tcap) return SB_ERR_SHAPE;
+    if (!aligned16(kc) || !aligned16(ks) || !aligned16(vc) || !aligned16(vs) || !aligned16(k) || !aligned16(v) || !aligned16(pos)) return SB_ERR_ALIGN;
+    return SB_OK;
+}
+
+const uint8_t* in_bytes(const void* p) { return static_cast<const uint8_t*>(p); }
+uint8_t* out_bytes(void* p) { return static_cast<uint8_t*>(p); }
+}  // namespace
+
+int sb_attn_kv4_store(const void* k, const void* v, void* kc, void* ks, void* vc, void* vs, const int* pos,
+                      int B, int Hkv, int n, int Tcap, int d, void* stream)
+{
+    if (int rc = check_kv4_rows(kc, ks, vc, vs, k, v, pos, B, Hkv, n, Tcap, d)) return rc;
+    hipError_t e = sb::launch_kv4_store(static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), out_bytes(kc), out_bytes(ks), out_bytes(vc), out_bytes(vs),
+                                        pos, B, Hkv, n, Tcap, d, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SB_OK : SB_ERR_LAUNCH;
+}
+
+int sb_attn_kv4_load(const void* kc, const void* ks, const void* vc, const void* vs, void* k, void* v, const int* pos,
+                     int B, int Hkv, int n, int Tcap, int d, void* stream)
+{
+    if (int rc = check_kv4_rows(kc, ks, vc, vs, k, v, pos, B, Hkv, n, Tcap, d)) return rc;
+    hipError_t e = sb::launch_kv4_load(in_bytes(kc), in_bytes(ks), in_bytes(vc), in_bytes(vs), static_cast<uint16_t*>(k), static_cast<uint16_t*>(v),
+                                       pos, B, Hkv, n, Tcap, d, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SB_OK : SB_ERR_LAUNCH;
+}
+
+namespace {
+int check_decode_kv4(int B, int H, int Hkv, int T, int Tcap, int d, bool scores)
+{
+    if (H < 1 || Hkv < 1 || H % Hkv != 0 || T < 1 || Tcap < T || T > sb::decode_max_T()) return SB_ERR_SHAPE;
+    if (int rc = check_kv4(B, Hkv, Tcap, d)) return rc;
+    if ((double)B * H > 16777215.0 || (double)B * H * (double)Tcap * d >= 1099511627776.0 || (scores && H / Hkv > sb::decode_kv4_most_group())) return SB_ERR_SHAPE;
+    return SB_OK;
+}
+}  // namespace
+
+size_t sb_attn_decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d, int scores)
+{
+    if (check_decode_kv4(B, H, Hkv, T, Tcap, d, scores != 0) != SB_OK) return 0;
+    return sb::decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, scores != 0);
+}
+
+int sb_attn_decode_kv4(const void* q, const void* kc, const void* ks, const void* vc, const void* vs, const void* r, const int* lens,
+                       const float* score, float* score_out, void* o, float* m, void* workspace, size_t workspace_bytes,
+                       int B, int H, int Hkv, int T, int Tcap, int d, void* stream)
+{
+    if (!q || !kc || !ks || !vc || !vs || !o || (score && !score_out)) return SB_ERR_NULL;
+    if (int rc = check_decode_kv4(B, H, Hkv, T, Tcap, d, score_out != nullptr)) return rc;
+    if (!aligned16(q) || !aligned16(kc) || !aligned16(ks) || !aligned16(vc) || !aligned16(vs) || !aligned16(r) || !aligned16(lens) ||
+        !aligned16(score) || !aligned16(score_out) || !aligned16(o) || !aligned16(m) || !aligned16(workspace))
+        return SB_ERR_ALIGN;
+    if (!workspace || workspace_bytes < sb::decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, score_out != nullptr)) return SB_ERR_WORKSPACE;
+    hipError_t e = sb::launch_decode_kv4(static_cast<const uint16_t*>(q), in_bytes(kc), in_bytes(ks), in_bytes(vc), in_bytes(vs), static_cast<const uint16_t*>(r),
+                                         lens, score, score_out, static_cast<uint16_t*>(o), m, static_cast<float*>(workspace),
+                                         B, H, Hkv, T, Tcap, d, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SB_OK : SB_ERR_LAUNCH;
+}
+
+namespace {
+int check_key_weight(int B, int H, int Hkv, int Tq, int T, int Tcap, int d)
+{
+    if (H < 1 || Hkv < 1 || H % Hkv != 0 || T < 1 || Tq < 1 || Tq > T || Tcap < T || T > sb::decode_max_T()) return SB_ERR_SHAPE;
+    if (int rc = check_cache(B, Hkv, Tcap, d)) return rc;
+    if ((double)B * H > 16777215.0 || (double)B * H * (double)Tq * d >= 1099511627776.0 || (double)((Tq + 31) / 32) * (H / Hkv) * B * Hkv >= 2147483648.0)
+        return SB_ERR_SHAPE;
+    return SB_OK;
+}
+}  // namespace
+
+size_t sb_attn_key_weight_workspace_bytes(int B, int H, int Hkv, int Tq, int T, int d)
+{
+    if (check_key_weight(B, H, Hkv, Tq, T, T, d) != SB_OK) return 0;
+    return sb::key_weight_workspace_bytes(B, H, Hkv, Tq, T);
+}
+
+int sb_attn_key_weight(const void* q, const void* k, const int* lens, const int* qlens, const float* score, float* score_out,
+                       void* workspace, size_t workspace_bytes, int B, int H, int Hkv, int Tq, int T, int Tcap, int d, void* stream)
+{
+    if (!q || !k || !score_out) return SB_ERR_NULL;
+    if (int rc = check_key_weight(B, H, Hkv, Tq, T, Tcap, d)) return rc;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(lens) || !aligned16(qlens) || !aligned16(score) || !aligned16(score_out) || !aligned16(workspace))
+        return SB_ERR_ALIGN;
+    if (!workspace || workspace_bytes < sb::key_weight_workspace_bytes(B, H, Hkv, Tq, T)) return SB_ERR_WORKSPACE;
+    hipError_t e = sb::launch_key_weight(static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), lens, qlens, score, score_out,
+                                         static_cast<float*>(workspace), B, H, Hkv, Tq, T, Tcap, d, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SB_OK : SB_ERR_LAUNCH;
+}
+
+namespace {
+bool overlap(const void* a, double a_bytes, const void* b, double b_bytes)
+{
+    const double x = (double)reinterpret_cast<uintptr_t>(a), y = (double)reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+}  // namespace
+
+int sb_attn_evict(const float* score, const int* lens, const void* const* src, void* const* dst, const int* row_bytes, int arrays,
+                  float* score_out, int* index, int* lens_out, int B, int Hkv, int T, int Tcap, int Tcap_out, int keep, int recent, void* stream)
+{
+    if (!score || !score_out || !index || !lens_out) return SB_ERR_NULL;
+    if (arrays < 0 || arrays > sb::EVICT_ARRAYS) return SB_ERR_SHAPE;
+    if (arrays > 0 && (!src || !dst || !row_bytes)) return SB_ERR_NULL;
+    for (int i = 0; i < arrays; ++i)
+        if (!src[i] || !dst[i]) return SB_ERR_NULL;
+    if (B < 1 || Hkv < 1 || (double)B * Hkv > 65535.0 || T < 1 || Tcap < T || Tcap > MOST_ROWS || Tcap_out > MOST_ROWS || keep < 1 || keep > Tcap_out ||
+        recent < 0 || recent > keep)
+        return SB_ERR_SHAPE;
+    if (!aligned16(score) || !aligned16(score_out) || !aligned16(index) || !aligned16(lens) || !aligned16(lens_out)) return SB_ERR_ALIGN;
+    const double rows = (double)B * Hkv * Tcap, rows_out = (double)B * Hkv * Tcap_out;
+    for (int i = 0; i < arrays; ++i) {
+        if (row_bytes[i] < 1 || row_bytes[i] > 65536) return SB_ERR_SHAPE;
+        if (!aligned16(src[i]) || !aligned16(dst[i])) return SB_ERR_ALIGN;
+    }
+    // rows move while others are still read
+    if (overlap(score, 4.0 * rows, score_out, 4.0 * rows_out) || (lens && overlap(lens, 4.0 * B, lens_out, 4.0 * B))) return SB_ERR_OVERLAP;
+    for (int i = 0; i < arrays; ++i)
+        for (int j = 0; j < arrays; ++j)
+            if (overlap(src[i], rows * row_bytes[i], dst[j], rows_out * row_bytes[j]) ||
+                (i < j && overlap(dst[i], rows_out * row_bytes[i], dst[j], rows_out * row_bytes[j])))
+                return SB_ERR_OVERLAP;
+    hipError_t e = sb::launch_evict(score, lens, src, dst, row_bytes, arrays, score_out, index, lens_out, B, Hkv, T, Tcap, Tcap_out, keep, recent,
+                                    static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SB_OK : SB_ERR_LAUNCH;
+}
+
 int sb_diag_mfma_rate(const void* operands, size_t operand_bytes, int iters, unsigned long long* ticks,
                       double* flop, void* stream)
 {
@@ -346,6 +495,7 @@ const char* sb_status_string(int status)
     case SB_ERR_ALIGN: return "pointer not 16-byte aligned";
     case SB_ERR_LAUNCH: return "kernel launch failed";
     case SB_ERR_WORKSPACE: return "workspace missing or too small";
+    case SB_ERR_OVERLAP: return "an output overlaps an input";
     default: return "unknown status";
     }
 }

@@ -1,0 +1,553 @@
+// Single-token decode on a 4-bit cache (sb_kv4.h): one new query per (entry, head) against the entry's keys and values, and the
+// weight that its heads give every key, added to the key's score.
+//
+// One pass over the cache, 2 (D / 2 + D / 32) bytes a key and kv head (136 at D = 128, 512 in bf16).  Chunks of keys combine as in
+// sb_decode.hip: a chunk's weights are taken as if nothing nearer were there, and are shifted afterwards by what the nearer chunks
+// took (Eq. 2).
+//   near launch      grid (kv head, block of query heads): the nearest keys, all of a short cache
+//   far launch       grid (chunk, kv head, block of query heads): the keys before those; returns at once where the nearest keys
+//                    have used up the stick (CARRY_EXHAUSTED: every farther weight is zero in fp32)
+//   combine launch   a workgroup per query head adds the chunks up in a fixed order; with scores, one per (kv head, chunk)
+//                    shifts the weights of its keys, sums them over the group's heads and adds the score
+//
+// A workgroup takes its keys from the nearest down in rounds of 32 per wave, wave 0 the nearest.
+//   logits   z[key][head] = K q: 16x16x32 bf16 MFMA, A = 16 rows of K, B = the query heads of the group.  A lane loads the D / 8
+//            bytes of its row that make up one A operand after the other (the order of the columns is free as long as q comes in
+//            the same one), and converts them in registers, the scale with them.
+//   weights  where the MFMA leaves the logits: a lane has four consecutive keys of one head, twice; the chain of Eq. 1's product
+//            over the four, their logarithm across the four lanes and the eight waves of a head (by LDS, one barrier a round).
+//   output   O^T[c][head] += V^T w: a lane's eight weights are the B operand as they lie; it loads D / 16 columns of those same
+//            eight rows of V, converts, and an in-register transposition (one v_perm per packed pair) makes the A operands.
+#include "sb_kernels.h"
+#include "sb_kv4.h"
+#include "sb_mma.h"
+
+namespace sb {
+namespace {
+
+constexpr int GMAX = 16;               // query heads of a group per workgroup: the columns of the MFMA
+constexpr int KW = 32;                 // keys per wave and round
+constexpr int NEAR_NW = 8, FAR_NW = 4;
+constexpr int NEAR = KW * NEAR_NW;     // keys of a near launch that has a far one behind it
+constexpr int ALONE = 2048;            // a cache is the near launch's alone up to here
+constexpr int MAXSLOT = 128;           // chunks, the nearest keys among them: two per lane of a wave
+constexpr long FAR_WGS = 4096;         // workgroups of the far launch, all heads together
+constexpr int MOST_GROUP = 1024;       // query heads of a kv head where scores are wanted
+constexpr int COMBINE_THREADS = 256;
+
+struct Args {
+    const uint16_t* q;
+    const uint8_t *kc, *ks, *vc, *vs;
+    const uint16_t* rb;
+    const int* lens;                   // rows per entry, or nullptr: T
+    const float* score;                // nullptr: zero
+    float* score_out;                  // nullptr: not wanted
+    uint16_t* o;
+    float* m;
+    float *part_o, *part_a;            // [heads][slots][D], [heads][slots]: slot 0 the nearest
+    float* wl;                         // [heads][Tcap]: weights inside their chunk, where scores are combined
+    int T, Tcap, Hkv, G, near, C, slots;
+};
+
+__device__ __forceinline__ int length_of(const Args& a, int b)
+{
+    return a.lens ? min(max(a.lens[b], 0), a.T) : a.T;
+}
+__device__ __forceinline__ int up32(int n) { return (n + 31) & ~31; }
+
+template <int CTRL> __device__ __forceinline__ float dpp(float x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
+// sum over the 16 lanes of a row, in all of them
+__device__ __forceinline__ float row_sum(float x)
+{
+    x += dpp<0xB1>(x);                 // quad_perm 1, 0, 3, 2
+    x += dpp<0x4E>(x);                 // quad_perm 2, 3, 0, 1
+    x += dpp<0x141>(x);                // row_half_mirror
+    return x + dpp<0x140>(x);          // row_mirror
+}
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x = row_sum(x);
+    float a, b;
+    both_halves(x + __shfl_xor(x, 16), a, b);
+    return a + b;
+}
+
+// `even`: v of this lane's column in row 0 (lanes 0 .. 31) or 2 (32 .. 63), `odd`: in row 1 or 3
+__device__ __forceinline__ void both_rows(float v, float& even, float& odd)
+{
+    auto sw = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), false, false);
+    even = __builtin_bit_cast(float, (int)sw[0]);
+    odd = __builtin_bit_cast(float, (int)sw[1]);
+}
+
+// what a lane loads of 32 keys
+template <int D> struct Tile {
+    typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+    uint32_t k[2][D / 32];             // row l16 (+ 16): columns lq D / 4 .. + D / 4 - 1
+    uint32_t ks[2];                    // and their scale
+    uint32_t v[8];                     // rows 16 (i / 4) + 4 lq + i % 4: columns D / 16 l16 .. + D / 16 - 1
+    uint32_t vs[2][D / 32];            // scales of four rows each, bytes as they lie
+};
+
+template <class V> __device__ __forceinline__ V load_as(const uint8_t* p)
+{
+    V x;
+    __builtin_memcpy(&x, p, sizeof(V));
+    return x;
+}
+
+template <int D> __device__ __forceinline__ void fetch(Tile<D>& t, const uint8_t* kc, const uint8_t* ks, const uint8_t* vc, const uint8_t* vs,
+                                                       int base, int l16, int lq)
+{
+    constexpr int ROW = D / 2, SROW = D / KV4_BLOCK;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int row = base + 16 * h + l16;
+        const uint8_t* p = kc + (long)row * ROW + lq * (ROW / 4);
+        if constexpr (D == 128) {
+            const u32x4 x = load_as<u32x4>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.k[h][i] = x[i];
+        } else if constexpr (D == 64) {
+            const uint2 x = load_as<uint2>(p);
+            t.k[h][0] = x.x;
+            t.k[h][1] = x.y;
+        } else {
+            t.k[h][0] = load_as<uint32_t>(p);
+        }
+        t.ks[h] = ks[(long)row * SROW + lq * SROW / 4];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint8_t* p = vc + (long)(base + 16 * (i / 4) + 4 * lq + i % 4) * ROW + l16 * (ROW / 16);
+        t.v[i] = D == 128 ? load_as<uint32_t>(p) : D == 64 ? load_as<uint16_t>(p) : *p;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint8_t* p = vs + (long)(base + 16 * h + 4 * lq) * SROW;
+        if constexpr (D == 128) {
+            const u32x4 x = load_as<u32x4>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.vs[h][i] = x[i];
+        } else if constexpr (D == 64) {
+            const uint2 x = load_as<uint2>(p);
+            t.vs[h][0] = x.x;
+            t.vs[h][1] = x.y;
+        } else {
+            t.vs[h][0] = load_as<uint32_t>(p);
+        }
+    }
+}
+
+// scale of row i of the eight, of this lane's columns (exponent bits; what stands below them does not count)
+template <int D> __device__ __forceinline__ uint32_t v_scale(const Tile<D>& t, int i, int l16)
+{
+    constexpr int PER = 128 / D;       // rows in a word
+    const int r = i % 4;
+    const uint32_t w = t.vs[i / 4][r / PER];
+    // byte of the row's first block: r % PER * D / 32; of this lane's block: + l16 D / 16 / 32
+    const int sh = 24 - 8 * ((r % PER) * (D / KV4_BLOCK)) - 8 * (l16 * (D / 16) / KV4_BLOCK);
+    return (w << sh) >> 1;
+}
+
+template <int D, bool FAR>
+__global__ void __launch_bounds__(64 * (FAR ? FAR_NW : NEAR_NW), 2)
+decode_kv4_kernel(const Args a)
+{
+    constexpr int NW = FAR ? FAR_NW : NEAR_NW;
+    constexpr int NTHR = 64 * NW;
+    constexpr int KEYS = KW * NW;          // keys per round
+    constexpr int CW = D / 16;             // columns of V per lane
+    constexpr int CH = D / 4;              // 16-byte chunks of a head's columns
+    __shared__ __attribute__((aligned(16))) float tot[2][GMAX][NW];      // per round parity: sp2 over a wave's keys
+    __shared__ __attribute__((aligned(16))) f32x4 ored[NW * GMAX * CH];
+
+    const int bkv = FAR ? blockIdx.y : blockIdx.x;     // entry * Hkv + kv head
+    const int g0 = blockIdx.z * GMAX;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, lq = lane >> 4;
+    const int b = bkv / a.Hkv;
+    const int len = length_of(a, b), end = up32(len);
+    const int slot = FAR ? (int)blockIdx.x + (a.near > 0) : 0;
+    const int top = FAR ? end - a.near - (int)blockIdx.x * a.C : end;
+    const int lo = max(0, FAR ? top - a.C : top - a.near);
+    const long hq0 = (long)bkv * a.G + g0;
+    const int live = min(GMAX, a.G - g0);
+    const long head = hq0 + min(l16, live - 1);
+    const float c2 = SB_LOG2E / sqrtf((float)D);
+
+    if constexpr (FAR) {
+        if (top <= 0) return;
+        if (!a.m && a.near > 0 && __builtin_amdgcn_ballot_w64(!(a.part_a[head * a.slots] >= CARRY_EXHAUSTED)) == 0) return;
+    }
+
+    const uint8_t* const kc = a.kc + (long)bkv * a.Tcap * (D / 2);
+    const uint8_t* const vc = a.vc + (long)bkv * a.Tcap * (D / 2);
+    const uint8_t* const ks = a.ks + (long)bkv * a.Tcap * (D / KV4_BLOCK);
+    const uint8_t* const vs = a.vs + (long)bkv * a.Tcap * (D / KV4_BLOCK);
+
+    bf16x8 qw[D / 32];                     // B operand: head l16 (columns past `live` repeat the last one)
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) qw[s] = *reinterpret_cast<const bf16x8*>(a.q + head * D + lq * (D / 4) + 8 * s);
+
+    f32x4 acc[CW];                         // O^T: row 4 lq + r of MFMA e is column CW (4 lq + r) + e, head l16
+#pragma unroll
+    for (int e = 0; e < CW; ++e) acc[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float carry = 0.0f;                    // sp2 of the keys already passed, head l16
+    const float odd_counts = (lq & 1) ? 0.0f : 1.0f, upper_counts = lq < 2 ? 1.0f : 0.0f;
+    int par = 0, hi = top;
+
+    // one round on the keys in t; whether another follows.  n: the next one's
+    auto round = [&](Tile<D>& t, Tile<D>& n) __attribute__((always_inline)) {
+        const int base = hi - KW * (wave + 1);             // this wave's keys; where that is below lo it has none, and loads the last ones
+        const int valid = base < lo ? 0 : len - base;
+        const bool more = hi - KEYS > lo;
+        if (more) fetch<D>(n, kc, ks, vc, vs, max(base - KEYS, lo), l16, lq);
+        // ---- logits, in base 2
+        f32x4 x[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+            const uint32_t s = t.ks[h] << 23;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const uint32_t w = t.k[h][i];
+                const u32x4 p = {kv4_pair<0>(w, s), kv4_pair<1>(w, s), kv4_pair<2>(w, s), kv4_pair<3>(w, s)};
+                z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p), qw[i], z, 0, 0, 0);
+            }
+            x[h] = z * c2;
+        }
+        if (valid < KW) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * h + 4 * lq + r >= valid) x[h][r] = -INFINITY;
+        }
+        // ---- the lane's chains: w[r] = e_r prod_{r' < r} (1 + e_r'), l = log2 of the whole product
+        float w[2][4], l[2];
+        float most = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float W = 1.0f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                w[h][r] = W * fast_exp2(x[h][r]);
+                W += w[h][r];
+            }
+            l[h] = fast_log2(W);
+            most += W;
+        }
+        // where a product overflows, w is the logarithm of the weight inside the lane
+        const bool logs = __builtin_amdgcn_ballot_w64(!(most < INFINITY)) != 0;
+        if (__builtin_expect(logs, 0)) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                l[h] = 0.0f;
+#pragma unroll
+                for (int r = 3; r >= 0; --r) {
+                    l[h] += sp2(x[h][r]);
+                    w[h][r] = x[h][r] - l[h];
+                }
+            }
+        }
+        // ---- across the lanes of a head: the row above of a pair, and the upper half, are nearer
+        float behind[2], sum[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float even, odd, lower, upper;
+            both_rows(l[h], even, odd);
+            both_halves(even + odd, lower, upper);
+            sum[h] = lower + upper;
+            behind[h] = __builtin_fmaf(odd, odd_counts, upper * upper_counts);
+        }
+        if (lq == 0) tot[par][l16][wave] = sum[0] + sum[1];
+        barrier_lds();
+        float above = carry;
+#pragma unroll
+        for (int j = 0; j < NW; j += 4) {
+            const f32x4 s = *reinterpret_cast<const f32x4*>(&tot[par][l16][j]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (j + i < wave) above += s[i];
+                carry += s[i];
+            }
+        }
+        // ---- weights
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float take = above + behind[h] + (h == 0 ? sum[1] : 0.0f);
+            if (__builtin_expect(logs, 0)) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[h][r] = fast_exp2(w[h][r] - take);
+            } else {
+                const float kf = fast_exp2(-(take + l[h]));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[h][r] *= kf;
+            }
+        }
+        if (a.score_out && base >= lo) {
+            if (a.wl) {
+                if (l16 < live)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        *reinterpret_cast<f32x4*>(a.wl + (hq0 + l16) * a.Tcap + base + 16 * h + 4 * lq) = f32x4{w[h][0], w[h][1], w[h][2], w[h][3]};
+            } else {
+                f32x4 s[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[h][r] = row_sum(l16 < live ? w[h][r] : 0.0f);
+                if (l16 < 2) {
+                    const int key = base + 16 * l16 + 4 * lq;
+                    const long at = (long)bkv * a.Tcap + key;
+                    const f32x4 mine = l16 ? s[1] : s[0];
+                    if (key + 4 <= len) {
+                        const f32x4 was = a.score ? *reinterpret_cast<const f32x4*>(a.score + at) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        *reinterpret_cast<f32x4*>(a.score_out + at) = was + mine;
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (key + r < len) a.score_out[at + r] = (a.score ? a.score[at + r] : 0.0f) + mine[r];
+                    }
+                }
+            }
+        }
+        // ---- output.  Weights as two bf16 (16 bits of mantissa): o itself is rounded to eight
+        bf16x8 w0, w1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            w0[i] = (__bf16)w[i / 4][i % 4];
+            w1[i] = (__bf16)(w[i / 4][i % 4] - (float)w0[i]);
+        }
+        uint32_t pv[8][(CW + 1) / 2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t s = v_scale<D>(t, i, l16);
+            if (valid < KW && 16 * (i / 4) + 4 * lq + i % 4 >= valid) s = 0x3f800000u;      // (whatever lies there, a zero weight makes it zero)
+            pv[i][0] = kv4_pair<0>(t.v[i], s);
+            if constexpr (CW >= 4) pv[i][1] = kv4_pair<1>(t.v[i], s);
+            if constexpr (CW >= 8) {
+                pv[i][2] = kv4_pair<2>(t.v[i], s);
+                pv[i][3] = kv4_pair<3>(t.v[i], s);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < CW; ++e) {
+            u32x4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                y[i] = __builtin_amdgcn_perm(pv[2 * i + 1][e >> 1], pv[2 * i][e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
+            const bf16x8 av = __builtin_bit_cast(bf16x8, y);
+            acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, w1, acc[e], 0, 0, 0);
+            acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, w0, acc[e], 0, 0, 0);
+        }
+        hi -= KEYS;
+        par ^= 1;
+        return more && (FAR || a.m || __builtin_amdgcn_ballot_w64(!(carry >= CARRY_EXHAUSTED)) != 0);
+    };
+    if (hi > lo) {
+        Tile<D> ta, tb;
+        fetch<D>(ta, kc, ks, vc, vs, max(hi - KW * (wave + 1), lo), l16, lq);
+        while (round(ta, tb) && round(tb, ta)) {}
+    }
+    // keys that no stick was left for keep their scores
+    if (!FAR && a.score_out && !a.wl && a.score_out != a.score)
+        for (int i = lo + tid; i < hi; i += NTHR) a.score_out[(long)bkv * a.Tcap + i] = a.score ? a.score[(long)bkv * a.Tcap + i] : 0.0f;
+    if (!FAR && a.wl && a.slots == 1)                      // (read by the combination)
+        for (int g = 0; g < live; ++g)
+            for (int i = lo + tid; i < hi; i += NTHR) a.wl[(hq0 + g) * a.Tcap + i] = 0.0f;
+
+    // ---- the waves' shares: a lane holds 4 CW columns of its head, CW chunks of 16 bytes, their places xor-ed with the head
+    if (l16 < live) {
+        f32x4* const r = ored + (wave * live + l16) * CH;
+#pragma unroll
+        for (int j = 0; j < CW; ++j) {
+            f32x4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = acc[(4 * j + i) % CW][(4 * j + i) / CW];
+            r[(CW * lq + j) ^ (l16 & 7)] = y;
+        }
+        if (wave == 0 && lq == 0) tot[par][l16][0] = carry;
+    }
+    barrier_lds();
+    for (int i = tid; i < live * CH; i += NTHR) {
+        const int g = i / CH, c = i % CH;
+        f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) s += ored[(w * live + g) * CH + (c ^ (g & 7))];
+        const float total = tot[par][g][0];
+        const long h = hq0 + g;
+        if (!FAR && (a.slots == 1 || (!a.m && total >= CARRY_EXHAUSTED))) {
+            typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+            if (a.rb) {
+                const float left = fast_exp2(-total);
+                const uint16_t* e = a.rb + ((bkv % a.Hkv) * (long)a.G + g0 + g) * D + 4 * c;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[k] += left * __builtin_bit_cast(float, (uint32_t)e[k] << 16);
+            }
+            *reinterpret_cast<bf16x4*>(a.o + h * D + 4 * c) = bf16x4{(__bf16)s[0], (__bf16)s[1], (__bf16)s[2], (__bf16)s[3]};
+            if (a.m && c == 0) a.m[h] = -total * SB_LN2;
+        }
+        if (a.part_o) {
+            *reinterpret_cast<f32x4*>(a.part_o + (h * a.slots + slot) * D + 4 * c) = s;
+            if (c == 0) a.part_a[h * a.slots + slot] = total;
+        }
+    }
+}
+
+// slots of an entry that hold keys
+__device__ __forceinline__ int slots_of(const Args& a, int end)
+{
+    return (a.near > 0) + (max(0, end - a.near) + a.C - 1) / a.C;
+}
+
+template <int D>
+__global__ void __launch_bounds__(COMBINE_THREADS)
+decode_kv4_combine_kernel(const Args a, int H, int heads)
+{
+    constexpr int NV = D / 4;              // a thread adds four columns of every NG-th slot
+    constexpr int NG = COMBINE_THREADS / NV;
+    __shared__ __attribute__((aligned(16))) float ored[NG][D];
+    __shared__ float f[MOST_GROUP];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if ((int)blockIdx.x < heads) {
+        const long bh = blockIdx.x;
+        const int n = slots_of(a, up32(length_of(a, (int)(bh / H))));
+        const float* pa = a.part_a + bh * a.slots;
+        if (!a.m && a.near > 0 && pa[0] >= CARRY_EXHAUSTED) return;    // finished by the near launch
+        if (a.slots == 1) return;                                      // (so is every head)
+        // slot i is shifted by everything the nearer (lower) slots took
+        float total = 0.0f;
+        for (int i = 0; i < n; ++i) {
+            if (tid == 0) f[i] = fast_exp2(-total);
+            total += pa[i];
+        }
+        __syncthreads();
+        const int c4 = tid % NV, grp = tid / NV;
+        f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = grp; i < n; i += NG) s += f[i] * *reinterpret_cast<const f32x4*>(a.part_o + (bh * a.slots + i) * D + 4 * c4);
+        *reinterpret_cast<f32x4*>(&ored[grp][4 * c4]) = s;
+        __syncthreads();
+        if (tid < D) {
+            float r = 0.0f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) r += ored[g][tid];
+            if (a.rb) r += fast_exp2(-total) * __builtin_bit_cast(float, (uint32_t)a.rb[(bh % H) * D + tid] << 16);
+            const __bf16 val = (__bf16)r;
+            a.o[bh * D + tid] = __builtin_bit_cast(uint16_t, val);
+            if (a.m && tid == 0) a.m[bh] = -total * SB_LN2;
+        }
+        return;
+    }
+    // ---- scores of one slot's keys
+    const int bkv = ((int)blockIdx.x - heads) / a.slots, slot = ((int)blockIdx.x - heads) % a.slots;
+    const int len = length_of(a, bkv / a.Hkv), end = up32(len);
+    if (slot >= slots_of(a, end)) return;
+    const bool is_near = a.near > 0 && slot == 0;
+    const int top = is_near ? end : end - a.near - (slot - (a.near > 0)) * a.C;
+    const int lo = max(0, top - (is_near ? a.near : a.C));
+    const long hq0 = (long)bkv * a.G;
+    bool any = false;
+    for (int g = wave; g < a.G; g += COMBINE_THREADS / 64) {
+        const float* pa = a.part_a + (hq0 + g) * a.slots;
+        float x = 0.0f;
+        for (int i = lane; i < slot; i += 64) x += pa[i];
+        x = wave_sum(x);
+        // the far launch left out the blocks of heads that are all exhausted
+        bool there = true;
+        if (!a.m && a.near > 0 && slot > 0) {
+            const int g0 = g / GMAX * GMAX;
+            there = __builtin_amdgcn_ballot_w64(!(a.part_a[(hq0 + min(g0 + (lane & 15), min(a.G, g0 + GMAX) - 1)) * a.slots] >= CARRY_EXHAUSTED)) != 0;
+        }
+        x = there ? fast_exp2(-x) : 0.0f;
+        any |= x != 0.0f;
+        if (lane == 0) f[g] = x;
+    }
+    if (!__syncthreads_or(any) && a.score_out == a.score) return;
+    for (int i = lo + tid; i < min(top, len); i += COMBINE_THREADS) {
+        float s = a.score ? a.score[(long)bkv * a.Tcap + i] : 0.0f;
+        for (int g = 0; g < a.G; ++g)
+            if (f[g] != 0.0f) s = __builtin_fmaf(f[g], a.wl[(hq0 + g) * a.Tcap + i], s);
+        a.score_out[(long)bkv * a.Tcap + i] = s;
+    }
+}
+
+struct Split {
+    int near, C, slots;
+};
+// The nearest keys in the near launch, the rest in chunks of whole rounds.  With m wanted every key is read whatever the nearest
+// ones take: they need no launch of their own.
+Split split_of(long wgs, int T, bool want_m)
+{
+    if (T <= ALONE) return {(T + 31) & ~31, KW * FAR_NW, 1};
+    Split s = {want_m ? 0 : NEAR, 0, 0};
+    constexpr int unit = KW * FAR_NW;
+    const int far = T + KW - 1 - s.near;
+    const long want = std::min((long)MAXSLOT - 1, std::max(1L, FAR_WGS / wgs));
+    s.C = (int)(((far + want - 1) / want + unit - 1) / unit * unit);
+    s.slots = (far + s.C - 1) / s.C + (s.near > 0);
+    return s;
+}
+
+Split split_for(int B, int H, int Hkv, int T, bool want_m)
+{
+    const int nz = (H / Hkv + GMAX - 1) / GMAX;
+    return split_of((long)B * Hkv * nz, T, want_m);
+}
+
+template <int D>
+hipError_t launch_d(Args a, int B, int H, float* workspace, hipStream_t stream)
+{
+    const long heads = (long)B * H;
+    const unsigned bkv = (unsigned)(B * a.Hkv), nz = (unsigned)((a.G + GMAX - 1) / GMAX);
+    const bool combine = a.slots > 1 || (a.score_out && a.G > GMAX);
+    if (combine) {
+        a.part_o = workspace;
+        a.part_a = a.part_o + heads * a.slots * D;
+        if (a.score_out) a.wl = a.part_a + ((heads * a.slots + 3) & ~3L);
+    }
+    hipError_t e = hipSuccess;
+    if (a.near > 0) {
+        hipLaunchKernelGGL((decode_kv4_kernel<D, false>), dim3(bkv, 1u, nz), dim3(64 * NEAR_NW), 0, stream, a);
+        if ((e = hipGetLastError()) != hipSuccess || !combine) return e;
+    }
+    if (a.slots > (a.near > 0)) {
+        hipLaunchKernelGGL((decode_kv4_kernel<D, true>), dim3((unsigned)(a.slots - (a.near > 0)), bkv, nz), dim3(64 * FAR_NW), 0, stream, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    const unsigned more = a.score_out ? bkv * (unsigned)a.slots : 0u;
+    hipLaunchKernelGGL((decode_kv4_combine_kernel<D>), dim3((unsigned)heads + more), dim3(COMBINE_THREADS), 0, stream, a, H, (int)heads);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int decode_kv4_most_group() { return MOST_GROUP; }
+
+// room for either split
+size_t decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d, bool scores)
+{
+    const long heads = (long)B * H;
+    const long slots = std::max(split_for(B, H, Hkv, T, false).slots, split_for(B, H, Hkv, T, true).slots);
+    size_t n = (size_t)heads * slots * d + (size_t)((heads * slots + 3) & ~3L);
+    if (scores) n += (size_t)heads * Tcap;
+    return sizeof(float) * n;
+}
+
+hipError_t launch_decode_kv4(const uint16_t* q, const uint8_t* kc, const uint8_t* ks, const uint8_t* vc, const uint8_t* vs, const uint16_t* rb,
+                             const int* lens, const float* score, float* score_out, uint16_t* o, float* m, float* workspace,
+                             int B, int H, int Hkv, int T, int Tcap, int d, hipStream_t stream)
+{
+    const Split s = split_for(B, H, Hkv, T, m != nullptr);
+    const Args a = {q, kc, ks, vc, vs, rb, lens, score, score_out, o, m, nullptr, nullptr, nullptr, T, Tcap, Hkv, H / Hkv, s.near, s.C, s.slots};
+    if (d == 32) return launch_d<32>(a, B, H, workspace, stream);
+    if (d == 64) return launch_d<64>(a, B, H, workspace, stream);
+    return launch_d<128>(a, B, H, workspace, stream);
+}
+
+}  // namespace sb

@@ -83,6 +83,32 @@ hipError_t launch_decode(const uint16_t* q, const uint16_t* k, const uint16_t* v
 size_t decode_static_bytes();
 hipError_t decode_static_scratch(float** out);
 
+// 4-bit cache (sb_kv4.h): rows k, v [B][Hkv][n][d] bf16 <-> codes [B][Hkv][Tcap][d / 2] and scales [B][Hkv][Tcap][d / 32],
+// rows pos[entry] .. + n - 1 of it (pos on the device, or nullptr: 0).
+hipError_t launch_kv4_store(const uint16_t* k, const uint16_t* v, uint8_t* kc, uint8_t* ks, uint8_t* vc, uint8_t* vs,
+                            const int* pos, int B, int Hkv, int n, int Tcap, int d, hipStream_t stream);
+hipError_t launch_kv4_load(const uint8_t* kc, const uint8_t* ks, const uint8_t* vc, const uint8_t* vs, uint16_t* k, uint16_t* v,
+                           const int* pos, int B, int Hkv, int n, int Tcap, int d, hipStream_t stream);
+
+// Single-token decode on a 4-bit cache, Tcap a multiple of 32.  lens: rows per entry on the device, or nullptr: T.
+// score, score_out: [B][Hkv][Tcap] or nullptr; workspace: decode_kv4_workspace_bytes bytes.
+int decode_kv4_most_group();               // query heads of a kv head, with scores
+size_t decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d, bool scores);
+hipError_t launch_decode_kv4(const uint16_t* q, const uint8_t* kc, const uint8_t* ks, const uint8_t* vc, const uint8_t* vs, const uint16_t* rb,
+                             const int* lens, const float* score, float* score_out, uint16_t* o, float* m, float* workspace,
+                             int B, int H, int Hkv, int T, int Tcap, int d, hipStream_t stream);
+
+// score_out = score + what the queries q [B][H][Tq][d], the last rows of their entries, give the keys k [B][Hkv][Tcap][d];
+// lens, qlens: rows and query rows per entry on the device, or nullptr: T, Tq.
+size_t key_weight_workspace_bytes(int B, int H, int Hkv, int Tq, int T);
+hipError_t launch_key_weight(const uint16_t* q, const uint16_t* k, const int* lens, const int* qlens, const float* score, float* score_out,
+                             float* workspace, int B, int H, int Hkv, int Tq, int T, int Tcap, int d, hipStream_t stream);
+
+// Rows that stay, of arrays [B][Hkv][Tcap][row_bytes] to [B][Hkv][Tcap_out][row_bytes]; src, dst, row_bytes are on the host.
+constexpr int EVICT_ARRAYS = 8;
+hipError_t launch_evict(const float* score, const int* lens, const void* const* src, void* const* dst, const int* row_bytes, int arrays,
+                        float* score_out, int* index, int* lens_out, int B, int Hkv, int T, int Tcap, int Tcap_out, int keep, int recent, hipStream_t stream);
+
 // MFMA-only diagnostic: operands = at least 1 MiB of bf16 on the device, ticks = 3 x u64 on the device
 hipError_t launch_diag_mfma(const void* operands, int iters, unsigned long long* ticks, hipStream_t stream);
 double diag_mfma_flop(int iters);

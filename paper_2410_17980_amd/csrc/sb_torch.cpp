@@ -52,6 +52,7 @@ const char* dtype_name(at::ScalarType t)
     case at::kFloat: return "torch.float32";
     case at::kInt: return "torch.int32";
     case at::kLong: return "torch.int64";
+    case at::kByte: return "torch.uint8";
     default: return c10::toString(t);
     }
 }
@@ -520,6 +521,244 @@ PyObject* decode(PyObject* const* a)
     return tuple({&o, &m});
 }
 
+const at::Tensor& on_gpu(PyObject* o, const char* name)
+{
+    const at::Tensor& t = tensor(o, name);
+    if (!t.is_cuda()) throw Failed(std::string(name) + " must live on the GPU");
+    return t;
+}
+
+// The tensors of a call on a cache: on one device, the current one where the call goes to its stream.
+class OneDevice {
+public:
+    explicit OneDevice(const Launch& on) : at_(on.device) {}
+    const at::Tensor& operator()(PyObject* o, const char* name)
+    {
+        const at::Tensor& t = on_gpu(o, name);
+        if (at_ < 0) at_ = t.device().index();
+        if (t.device().index() != at_) throw Failed(std::string(name) + " is on another device than the call");
+        return t;
+    }
+    void* operator()(PyObject* o, at::ScalarType dtype, at::IntArrayRef shape, const char* name)
+    {
+        if (none(o)) return nullptr;
+        (*this)(o, name);
+        return ptr(o, dtype, shape, name);
+    }
+
+private:
+    c10::DeviceIndex at_;
+};
+
+constexpr at::ScalarType U8 = at::kByte, I32 = at::kInt;
+
+// [B, Hkv, Tcap, d] of a 4-bit cache
+struct Cache4 {
+    int B, Hkv, Tcap, d;
+    void *kc, *ks, *vc, *vs;
+};
+Cache4 cache4(PyObject* kc, PyObject* ks, PyObject* vc, PyObject* vs, OneDevice& dev)
+{
+    const at::Tensor& t = dev(kc, "kc");
+    if (t.dim() != 4) throw Failed("kc: expected [B, Hkv, Tcap, d / 2]");
+    Cache4 c;
+    c.B = dim(t, 0); c.Hkv = dim(t, 1); c.Tcap = dim(t, 2);
+    c.d = dim(t, 3) > INT32_MAX / 2 ? INT32_MAX : 2 * dim(t, 3);
+    const Shape codes = {c.B, c.Hkv, c.Tcap, c.d / 2}, scales = {c.B, c.Hkv, c.Tcap, c.d / 32};
+    c.kc = dev(kc, U8, codes, "kc");
+    c.ks = dev(ks, U8, scales, "ks");
+    c.vc = dev(vc, U8, codes, "vc");
+    c.vs = dev(vs, U8, scales, "vs");
+    if (!c.ks || !c.vc || !c.vs) throw Failed("codes and scales of k and v are required");
+    return c;
+}
+
+// kv4_store(k, v, kc, ks, vc, vs, pos, stream)
+PyObject* kv4_store(PyObject* const* a)
+{
+    on_gpu(a[2], "kc");
+    const Launch on = launch_on(a[7]);
+    OneDevice dev(on);
+    const Cache4 c = cache4(a[2], a[3], a[4], a[5], dev);
+    const at::Tensor& tk = dev(a[0], "k");
+    if (tk.dim() != 4) throw Failed("k: expected [B, Hkv, n, d]");
+    const int n = dim(tk, 2);
+    const Shape rows = {c.B, c.Hkv, n, c.d}, entries = {c.B};
+    void* k = dev(a[0], BF, rows, "k");
+    void* v = dev(a[1], BF, rows, "v");
+    auto* pos = static_cast<const int*>(dev(a[6], I32, entries, "pos"));
+    call("sb_attn_kv4_store", [&] { return sb_attn_kv4_store(k, v, c.kc, c.ks, c.vc, c.vs, pos, c.B, c.Hkv, n, c.Tcap, c.d, on.stream); });
+    Py_RETURN_NONE;
+}
+
+// kv4_load(kc, ks, vc, vs, n, pos, k, v, stream)
+PyObject* kv4_load(PyObject* const* a)
+{
+    on_gpu(a[0], "kc");
+    const Launch on = launch_on(a[8]);
+    OneDevice dev(on);
+    const Cache4 c = cache4(a[0], a[1], a[2], a[3], dev);
+    const int n = to_int(a[4]);
+    if (n < 1 || n > c.Tcap) throw Failed("n: expected 1 .. Tcap");
+    const Shape rows = {c.B, c.Hkv, n, c.d}, entries = {c.B};
+    auto* pos = static_cast<const int*>(dev(a[5], I32, entries, "pos"));
+    if (!none(a[6])) dev(a[6], "k");
+    if (!none(a[7])) dev(a[7], "v");
+    const at::Tensor& like = THPVariable_Unpack(a[0]);
+    Out k(a[6], BF, rows, like, "k", on), v(a[7], BF, rows, like, "v", on);
+    call("sb_attn_kv4_load", [&] { return sb_attn_kv4_load(c.kc, c.ks, c.vc, c.vs, k.p(), v.p(), pos, c.B, c.Hkv, n, c.Tcap, c.d, on.stream); });
+    return tuple({&k, &v});
+}
+
+// decode_kv4(q, kc, ks, vc, vs, T, lens, r, score, score_out, o, m, want_m, workspace, stream)
+PyObject* decode_kv4(PyObject* const* a)
+{
+    on_gpu(a[1], "kc");
+    const Launch on = launch_on(a[14]);
+    OneDevice dev(on);
+    const Cache4 c = cache4(a[1], a[2], a[3], a[4], dev);
+    const at::Tensor& tq = dev(a[0], "q");
+    if (tq.dim() != 3) throw Failed("q: expected [B, H, d]");
+    const int H = dim(tq, 1);
+    const int T = none(a[5]) ? c.Tcap : to_int(a[5]);
+    const Shape sq = {c.B, H, c.d}, sr = {H, c.d}, sm = {c.B, H}, entries = {c.B}, scores = {c.B, c.Hkv, c.Tcap};
+    void* q = dev(a[0], BF, sq, "q");
+    auto* lens = static_cast<const int*>(dev(a[6], I32, entries, "lens"));
+    void* r = dev(a[7], BF, sr, "r");
+    auto* score = static_cast<const float*>(dev(a[8], F32, scores, "score"));
+    PyObject* given = none(a[9]) ? a[8] : a[9];
+    auto* score_out = static_cast<float*>(dev(given, F32, scores, "score_out"));
+    for (int i : {10, 11, 13})
+        if (!none(a[i])) dev(a[i], i == 10 ? "o" : i == 11 ? "m" : "workspace");
+    const bool want_m = !none(a[11]) || truth(a[12]);
+    Out o(a[10], BF, sq, tq, "o", on);
+    auto go = [&](float* m) {
+        Workspace ws(a[13], sb_attn_decode_kv4_workspace_bytes(c.B, H, c.Hkv, T, c.Tcap, c.d, score_out != nullptr), tq, on);
+        call("sb_attn_decode_kv4", [&] {
+            return sb_attn_decode_kv4(q, c.kc, c.ks, c.vc, c.vs, r, lens, score, score_out, o.p(), m, ws.p(), ws.bytes(),
+                                      c.B, H, c.Hkv, T, c.Tcap, c.d, on.stream);
+        });
+    };
+    if (!want_m) {
+        go(nullptr);
+        if (!score_out) return o.take();
+        Out s(given, F32, scores, tq, "score_out", on);
+        return tuple({&o, &s});
+    }
+    Out m(a[11], F32, sm, tq, "m", on);
+    go(m.p<float>());
+    if (!score_out) return tuple({&o, &m});
+    Out s(given, F32, scores, tq, "score_out", on);
+    return tuple({&o, &m, &s});
+}
+
+// key_weight(q, k, T, lens, qlens, score, score_out, workspace, stream)
+PyObject* key_weight(PyObject* const* a)
+{
+    on_gpu(a[0], "q");
+    const Launch on = launch_on(a[8]);
+    OneDevice dev(on);
+    const at::Tensor& tq = dev(a[0], "q");
+    const at::Tensor& tk = dev(a[1], "k");
+    if (tq.dim() != 4 || tk.dim() != 4) throw Failed("expected a [B, H, T, d] tensor");
+    const int B = dim(tq, 0), H = dim(tq, 1), Tq = dim(tq, 2), d = dim(tq, 3), Hkv = dim(tk, 1), Tcap = dim(tk, 2);
+    const int T = none(a[2]) ? Tcap : to_int(a[2]);
+    const Shape sq = {B, H, Tq, d}, sk = {B, Hkv, Tcap, d}, entries = {B}, scores = {B, Hkv, Tcap};
+    void* q = dev(a[0], BF, sq, "q");
+    void* k = dev(a[1], BF, sk, "k");
+    auto* lens = static_cast<const int*>(dev(a[3], I32, entries, "lens"));
+    auto* qlens = static_cast<const int*>(dev(a[4], I32, entries, "qlens"));
+    auto* score = static_cast<const float*>(dev(a[5], F32, scores, "score"));
+    PyObject* given = none(a[6]) ? a[5] : a[6];
+    if (!none(given)) dev(given, "score_out");
+    if (!none(a[7])) dev(a[7], "workspace");
+    Out out(given, F32, scores, tq, "score_out", on);
+    Workspace ws(a[7], sb_attn_key_weight_workspace_bytes(B, H, Hkv, Tq, T, d), tq, on);
+    call("sb_attn_key_weight", [&] {
+        return sb_attn_key_weight(q, k, lens, qlens, score, out.p<float>(), ws.p(), ws.bytes(), B, H, Hkv, Tq, T, Tcap, d, on.stream);
+    });
+    return out.take();
+}
+
+// evict(score, rows, keep, recent, T, lens, out, score_out, lens_out, index, stream)
+PyObject* evict(PyObject* const* a)
+{
+    constexpr Py_ssize_t MOST = 8;
+    on_gpu(a[0], "score");
+    const Launch on = launch_on(a[10]);
+    OneDevice dev(on);
+    const at::Tensor& ts = dev(a[0], "score");
+    if (ts.dim() != 3) throw Failed("score: expected [B, Hkv, Tcap]");
+    const int B = dim(ts, 0), Hkv = dim(ts, 1), Tcap = dim(ts, 2);
+    const int keep = to_int(a[2]), recent = to_int(a[3]), T = none(a[4]) ? Tcap : to_int(a[4]);
+    const Py_ssize_t n = PyTuple_Size(a[1]);
+    if (n < 0) throw Raised{};
+    if (n > MOST) throw Failed("rows: at most 8 tensors");
+    if (!none(a[6]) && PyTuple_Size(a[6]) != n) throw Failed("out: expected as many tensors as rows");
+    if (keep < 1) throw Failed("keep: expected 1 or more");
+    // room of the outputs: that of the first one given, or as in rows
+    int cap = Tcap;
+    if (!none(a[6]) && n > 0) {
+        const at::Tensor& t = dev(PyTuple_GET_ITEM(a[6], 0), "out");
+        if (t.dim() < 3) throw Failed("out: expected [B, Hkv, Tcap_out, ...]");
+        cap = dim(t, 2);
+    } else if (!none(a[7])) {
+        const at::Tensor& t = dev(a[7], "score_out");
+        if (t.dim() != 3) throw Failed("score_out: expected [B, Hkv, Tcap_out]");
+        cap = dim(t, 2);
+    }
+    if (keep > cap) throw Failed("keep: more rows than there is room for");
+    const Shape entries = {B}, in_s = {B, Hkv, Tcap}, out_s = {B, Hkv, cap}, kept = {B, Hkv, keep};
+    auto* score = static_cast<const float*>(dev(a[0], F32, in_s, "score"));
+    auto* lens = static_cast<const int*>(dev(a[5], I32, entries, "lens"));
+    for (int i : {7, 8, 9})
+        if (!none(a[i])) dev(a[i], i == 7 ? "score_out" : i == 8 ? "lens_out" : "index");
+    const void* src[MOST];
+    void* dst[MOST];
+    int row_bytes[MOST];
+    c10::SmallVector<at::Tensor, MOST> outs;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::Tensor& t = dev(PyTuple_GET_ITEM(a[1], i), "rows");
+        if (t.dim() < 3 || t.size(0) != B || t.size(1) != Hkv || t.size(2) != Tcap)
+            throw Failed("rows have shape " + text(t.sizes()) + ", expected [B, Hkv, Tcap, ...] of score");
+        if (!t.is_contiguous()) throw Failed("rows must be contiguous");
+        int64_t bytes = t.element_size();
+        Shape so;
+        for (int64_t j = 0; j < t.dim(); ++j) {
+            so.push_back(j == 2 ? cap : t.size(j));
+            if (j > 2) bytes *= t.size(j);
+        }
+        if (bytes < 1 || bytes > 65536) throw Failed("rows: expected 1 .. 65536 bytes a row");
+        row_bytes[i] = (int)bytes;
+        src[i] = t.data_ptr();
+        if (none(a[6])) {
+            outs.push_back(allocate(so, t.scalar_type(), t, on, true));
+        } else {
+            PyObject* given = PyTuple_GET_ITEM(a[6], i);
+            dev(given, "out");
+            ptr(given, t.scalar_type(), so, "out");
+            outs.push_back(THPVariable_Unpack(given));
+        }
+        dst[i] = outs.back().data_ptr();
+    }
+    Out score_out(a[7], F32, out_s, ts, "score_out", on), lens_out(a[8], I32, entries, ts, "lens_out", on), index(a[9], I32, kept, ts, "index", on);
+    call("sb_attn_evict", [&] {
+        return sb_attn_evict(score, lens, src, dst, row_bytes, (int)n, score_out.p<float>(), index.p<int>(), lens_out.p<int>(), B, Hkv, T, Tcap, cap,
+                             keep, recent, on.stream);
+    });
+    PyObject* out = PyTuple_New(n);
+    if (!out) throw Raised{};
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject* o = THPVariable_Wrap(outs[i]);
+        if (!o) {
+            Py_DECREF(out);
+            throw Raised{};
+        }
+        PyTuple_SET_ITEM(out, i, o);
+    }
+    return Py_BuildValue("(NNNN)", out, score_out.take(), lens_out.take(), index.take());
+}
+
 // set_errors(SbAttnError, torch.cuda.OutOfMemoryError)
 PyObject* set_errors(PyObject* const* a)
 {
@@ -558,6 +797,7 @@ PyMethodDef methods[] = {
     SB_ENTRY(set_errors, 2), SB_ENTRY(forward, 10), SB_ENTRY(halt, 7), SB_ENTRY(forward_f32, 7),
     SB_ENTRY(backward, 14), SB_ENTRY(backward_dq, 8), SB_ENTRY(backward_dkdv, 8),
     SB_ENTRY(varlen_forward, 10), SB_ENTRY(varlen_backward, 14), SB_ENTRY(decode, 11),
+    SB_ENTRY(kv4_store, 8), SB_ENTRY(kv4_load, 9), SB_ENTRY(decode_kv4, 15), SB_ENTRY(key_weight, 9), SB_ENTRY(evict, 11),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_sbtorch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
