@@ -75,6 +75,24 @@ __device__ __forceinline__ float wave_sum(float x)
     return a + b;
 }
 
+// sum over the lanes below this one, and over all in `total`
+template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_or_zero(float x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ float wave_prefix(float v, float& total)
+{
+    float inc = v;
+    inc += dpp_or_zero<0x111, 0xF>(inc);                  // row_shr:1, 2, 4, 8
+    inc += dpp_or_zero<0x112, 0xF>(inc);
+    inc += dpp_or_zero<0x114, 0xF>(inc);
+    inc += dpp_or_zero<0x118, 0xF>(inc);
+    inc += dpp_or_zero<0x142, 0xA>(inc);                  // row_bcast:15 into rows 1 and 3
+    inc += dpp_or_zero<0x143, 0xC>(inc);                  // row_bcast:31 into rows 2 and 3
+    total = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inc), 63));
+    return inc - v;
+}
+
 // `even`: v of this lane's column in row 0 (lanes 0 .. 31) or 2 (32 .. 63), `odd`: in row 1 or 3
 __device__ __forceinline__ void both_rows(float v, float& even, float& odd)
 {
@@ -422,15 +440,26 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
         if (!a.m && a.near > 0 && pa[0] >= CARRY_EXHAUSTED) return;    // finished by the near launch
         if (a.slots == 1) return;                                      // (so is every head)
         // slot i is shifted by everything the nearer (lower) slots took
-        float total = 0.0f;
-        for (int i = 0; i < n; ++i) {
-            if (tid == 0) f[i] = fast_exp2(-total);
-            total += pa[i];
+        const int c4 = tid % NV, grp = tid / NV;
+        const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + bh * a.slots * D) + c4;
+        // all of a thread's share is in flight at once
+        constexpr int N = MAXSLOT / NG;
+        f32x4 x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = grp + i * NG < n ? po[(grp + i * NG) * NV] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        float p[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) p[e] = 2 * lane + e < n ? pa[2 * lane + e] : 0.0f;
+        float total;
+        const float before = wave_prefix(p[0] + p[1], total);
+        if (wave == 0) {
+            f[2 * lane] = 2 * lane < n ? fast_exp2(-before) : 0.0f;
+            f[2 * lane + 1] = 2 * lane + 1 < n ? fast_exp2(-(before + p[0])) : 0.0f;
         }
         __syncthreads();
-        const int c4 = tid % NV, grp = tid / NV;
         f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int i = grp; i < n; i += NG) s += f[i] * *reinterpret_cast<const f32x4*>(a.part_o + (bh * a.slots + i) * D + 4 * c4);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s += f[grp + i * NG] * x[i];
         *reinterpret_cast<f32x4*>(&ored[grp][4 * c4]) = s;
         __syncthreads();
         if (tid < D) {

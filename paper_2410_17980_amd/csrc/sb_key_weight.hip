@@ -1,10 +1,16 @@
 // The weight that a prompt's queries give each key: score_out[i] = score[i] + sum over query rows j and heads of the group of A[i,j]
 // (Eq. 1).  The queries are the last rows of their entry, all of it or a window at its end.
 //
-// Logits and weights as in the forward; in place of A V the sum of A over the queries.  A unit is 32 query rows of one head; units of
-// the heads of a group at the same rows are neighbours, as they read the same keys.  A workgroup takes NW units, sweeps 64-key tiles
-// from the last unit's diagonal towards key 0, and leaves the sums over its queries, one number a key, in the workspace; a second
-// launch adds the workgroups up in a fixed order.  It stops where the stick of all its rows is used up (CARRY_EXHAUSTED), and notes how far it came.
+// Logits as in the forward, S^T = K Q^T by the 32x32x16 MFMA, a lane 16 keys of one query; Eq. 1's product along the keys in the lane,
+// and what is left of a query's stick carried from 32 keys to the next as it is, not by its logarithm: a weight here is a result in
+// fp32, and the logarithm of a carry around 30 would be off by 2^-20 of it (the forward's weights go on to a product in bf16).  From
+// less than 2^-126 of the stick on, no weight is more than a subnormal number: the row counts as exhausted and what is farther gets nothing from it.
+// In place of A V the sum of A over the queries.  A unit is 32 query rows of one head; units of the heads of a group at the
+// same rows are neighbours, as they read the same keys.  What a workgroup's queries give the keys, one number a key, goes into
+// the workspace, with how far it reaches; a last launch adds the workgroups up in a fixed order.
+//   key_weight_kernel        NW units a workgroup, 64-key tiles through LDS for all of them, from the last unit's diagonal towards key 0
+//   key_weight_small_kernel  one unit a workgroup, its waves 32 keys each, side by side; where there are few units, also split over
+//                            chunks of keys: a first launch finds what each chunk leaves of the sticks, a second one the weights
 #include "sb_kernels.h"
 #include "sb_mma.h"
 
@@ -12,8 +18,9 @@ namespace sb {
 namespace {
 
 constexpr int NW = 4;                  // waves of a workgroup, a unit each
+constexpr int SNW = 8;                 // waves of a small kernel's workgroup
 constexpr int TK = 64;                 // keys of a tile
-constexpr int SUM_THREADS = 256;
+constexpr int SUM_THREADS = 512;
 
 template <int CTRL> __device__ __forceinline__ float dpp(float x)
 {
@@ -47,9 +54,10 @@ struct Args {
     const int *lens, *qlens;           // or nullptr: T, Tq
     const float* score;                // or nullptr: zero
     float* score_out;
-    float* part;                       // [entry * kv head][workgroup][Tpad]
-    int* reach;                        // [entry * kv head][workgroup][2]: first key written, one past the last
-    int H, Hkv, G, Tq, T, Tcap, Tpad, groups;
+    float* part;                       // [entry * kv head][group][Tpad]; a group is a workgroup's units
+    int* reach;                        // [entry * kv head][group][chunks][2]: first key written, one past the last
+    float* left;                       // [entry * kv head][unit][chunks][32]: the share of the stick that a chunk leaves of each query's
+    int H, Hkv, G, Tq, T, Tcap, Tpad, groups, chunks, C;
 };
 
 __device__ __forceinline__ int length_of(const int* lens, int b, int most)
@@ -57,13 +65,121 @@ __device__ __forceinline__ int length_of(const int* lens, int b, int most)
     return lens ? min(max(lens[b], 0), most) : most;
 }
 
+constexpr float LEAST = 0x1p-126f;     // of the stick
+__device__ __forceinline__ bool none_left(float stick) { return __builtin_amdgcn_ballot_w64(!(stick < LEAST)) == 0; }
+
+// One query's share of a subtile of 32 keys, a half-wave 16 of them: with the stick whole before its nearest key, the weight of
+// key r is w[r] * mine, and `all` is what the 32 leave.  MASK: keys from `visible` on are not seen.
+template <bool MASK>
+__device__ __forceinline__ void weights(const f32x16& s, float c2, int visible, int hh, float (&w)[16], float& mine, float& all)
+{
+    // w[r] = W_r e_r, W_{r+1} = W_r + w[r], e = sigma / (1 - sigma): W_r = prod_{r' < r} 1 / (1 - sigma_r')
+    float W = 1.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        float e = fast_exp2(s[r] * c2);
+        if (MASK) e = r < visible ? e : 0.0f;
+        w[r] = W * e;
+        W += w[r];
+    }
+    float lo, hi;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(W < 0x1p120f)) == 0, 1)) {
+        both_halves(__builtin_amdgcn_rcpf(W), lo, hi);
+        all = lo * hi;
+        mine = hh ? hi : all;
+        return;
+    }
+    // in the log form
+    float run = 0.0f;
+#pragma unroll
+    for (int r = 15; r >= 0; --r) {
+        const float x = !MASK || r < visible ? s[r] * c2 : -INFINITY;
+        run += sp2(x);
+        w[r] = x - run;
+    }
+    both_halves(run, lo, hi);
+    const float take = hh ? 0.0f : hi;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w[r] = fast_exp2(w[r] - take);
+    mine = 1.0f;
+    all = fast_exp2(-(lo + hi));
+}
+
+// the unit's rows and what they see
+struct Unit {
+    int head, strip, sees, all, some;  // this lane's query sees the keys below `sees`, all of the unit's those below `all`, one at least those below `some`
+    bool there;
+};
+__device__ __forceinline__ Unit unit_of(const Args& a, int unit, int bkv, int off, int qlen, int n)
+{
+    Unit u;
+    u.strip = unit / a.G;
+    u.head = (bkv % a.Hkv) * a.G + unit % a.G;
+    const int row = 32 * u.strip + n;
+    u.there = row < qlen;
+    u.sees = u.there ? off + row : 0;
+    u.all = max(0, off + 32 * u.strip);
+    u.some = 32 * u.strip < qlen ? max(0, off + min(32 * u.strip + 32, qlen) - 1) : 0;
+    return u;
+}
+
+template <int D> struct Cfg {
+    static constexpr int ROW = 2 * D, CPR = ROW / 16, BLK_ROWS = 1024 / ROW;
+    static constexpr int SUB = 32 * ROW;                // bytes of 32 rows
+    static constexpr int LOADS = SUB / 1024;            // loads of a wave for 32 rows
+};
+
+// 32 rows to LDS, swizzled, those past `last` as that one; every lane's offsets in off
+template <int D> __device__ __forceinline__ void sub_offsets(int (&off)[Cfg<D>::LOADS], int lane)
+{
+    using C = Cfg<D>;
+#pragma unroll
+    for (int i = 0; i < C::LOADS; ++i) {
+        const int r = i * C::BLK_ROWS + lane / C::CPR;
+        off[i] = r * C::ROW + (((lane % C::CPR) ^ swz_perm<D>(r)) << 4);
+    }
+}
+template <int D> __device__ __forceinline__ void sub_to_lds(const uint16_t* src, const int (&off)[Cfg<D>::LOADS], int last, const char* dst, int lane)
+{
+    using C = Cfg<D>;
+    if (last >= 31) dma16_to_lds_run(src, off, dst);
+    else {
+        int o[C::LOADS];
+#pragma unroll
+        for (int i = 0; i < C::LOADS; ++i) o[i] = off[i] - max(i * C::BLK_ROWS + lane / C::CPR - last, 0) * C::ROW;
+        dma16_to_lds_run(src, o, dst);
+    }
+}
+
+// B operand of the logits from 32 rows of q in LDS; zero where there is no row: what lies there may be anything
+template <int D> __device__ __forceinline__ void read_q(bf16x8 (&qf)[D / 16], uint32_t at, int n, int hh, bool there)
+{
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+        u32x4 y = lds_load16(at + tile_off_perm<D>(n, 2 * s + hh));
+        if (!there) y = u32x4{0u, 0u, 0u, 0u};
+        qf[s] = __builtin_bit_cast(bf16x8, y);
+    }
+}
+
+template <int D> __device__ __forceinline__ f32x16 logits(const bf16x8 (&qf)[D / 16], const uint32_t (&aoff)[D / 16], uint32_t at)
+{
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lds_load16(aoff[i] + at)), qf[i], s, 0, 0, 0);
+    return s;
+}
+
 template <int D>
 __global__ void __launch_bounds__(64 * NW, 2)
 key_weight_kernel(const Args a, int BHkv, int first_wg)
 {
-    constexpr int ROW = 2 * D, CPR = ROW / 16, BLK_ROWS = 1024 / ROW;
-    constexpr int TILE = TK * ROW, NPW = TILE / 1024 / NW;
-    __shared__ __attribute__((aligned(1024))) char tiles[2 * TILE];
+    using C = Cfg<D>;
+    constexpr int TILE = 2 * C::SUB, NPW = TILE / 1024 / NW;
+    __shared__ __attribute__((aligned(1024))) char tiles[NW * C::SUB];      // two of K; before that, the units' q
     __shared__ __attribute__((aligned(16))) float csum[2][NW][TK];
     __shared__ __attribute__((aligned(16))) int s_done[2][NW];
 
@@ -76,14 +192,7 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     const int len = length_of(a.lens, b, a.T), qlen = length_of(a.qlens, b, a.Tq);
     const int off = len - qlen;                                         // position of query row 0
     int* const reach = a.reach + ((long)bkv * a.groups + grp) * 2;
-
-    const int unit = grp * NW + wave;
-    const int strip = unit / a.G, head = (bkv % a.Hkv) * a.G + unit % a.G;
-    // keys below `sees` are visible to this lane's query; to all of the strip's below `all`, to one at least below `some`
-    const int row = 32 * strip + n;
-    const int sees = row < qlen ? off + row : 0;
-    const int all = max(0, off + 32 * strip);
-    const int some = 32 * strip < qlen ? max(0, off + min(32 * strip + 32, qlen) - 1) : 0;
+    const Unit u = unit_of(a, grp * NW + wave, bkv, off, qlen, n);
     const int last_strip = min((grp * NW + NW - 1) / a.G, (qlen - 1) / 32);            // of the workgroup, with rows in it
     const int top = grp * NW / a.G * 32 < qlen ? max(0, off + min(32 * last_strip + 32, qlen) - 1) : 0;
     if (top == 0) {
@@ -92,36 +201,35 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     }
 
     const float c2 = SB_LOG2E / sqrtf((float)D);
-    bf16x8 qf[D / 16];                         // zero where there is no row: what lies there may be anything
+    const uint32_t smem0 = lds_offset(tiles);
+    bf16x8 qf[D / 16];
     {
-        const uint16_t* x = a.q + (((long)b * a.H + head) * a.Tq + min(row, a.Tq - 1)) * D + 8 * hh;
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            u32x4 y = *reinterpret_cast<const u32x4*>(x + 16 * s);
-            if (row >= qlen) y = u32x4{0u, 0u, 0u, 0u};
-            qf[s] = __builtin_bit_cast(bf16x8, y);
-        }
+        int qoff[C::LOADS];
+        sub_offsets<D>(qoff, lane);
+        const int r0 = min(32 * u.strip, (a.Tq - 1) / 32 * 32);
+        sub_to_lds<D>(a.q + (((long)b * a.H + u.head) * a.Tq + r0) * D, qoff, a.Tq - 1 - r0, tiles + wave * C::SUB, lane);
+        dma_wait<0>();
+        read_q<D>(qf, smem0 + wave * C::SUB, n, hh, u.there);
+        barrier_lds();
     }
     const uint16_t* const kg = reinterpret_cast<const uint16_t*>(scalar_base(a.k + (long)bkv * a.Tcap * D));
     int goff[NPW];
 #pragma unroll
     for (int i = 0; i < NPW; ++i) {
-        const int r = (wave * NPW + i) * BLK_ROWS + lane / CPR;
-        goff[i] = r * ROW + (((lane % CPR) ^ swz_perm<D>(r)) << 4);
+        const int r = (wave * NPW + i) * C::BLK_ROWS + lane / C::CPR;
+        goff[i] = r * C::ROW + (((lane % C::CPR) ^ swz_perm<D>(r)) << 4);
     }
     auto stage = [&](int jt, int st) __attribute__((always_inline)) {
         const uint16_t* src = kg + (long)jt * TK * D;
         char* dst = tiles + st * TILE + wave * NPW * 1024;
         if ((jt + 1) * TK <= len) dma16_to_lds_run(src, goff, dst);
-        else dma16_to_lds_run_clamped<ROW, BLK_ROWS>(src, goff, wave * NPW * BLK_ROWS + lane / CPR, len - 1 - jt * TK, dst);
+        else dma16_to_lds_run_clamped<C::ROW, C::BLK_ROWS>(src, goff, wave * NPW * C::BLK_ROWS + lane / C::CPR, len - 1 - jt * TK, dst);
     };
-    const uint32_t smem0 = lds_offset(tiles);
     uint32_t aoff[D / 16];
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) aoff[s] = smem0 + tile_off_perm<D>(perm_row(n), 2 * s + hh);
 
-    // a row that is not there has nothing of its stick left
-    float carry = row < qlen ? 0.0f : 1e9f;
+    float stick = u.there ? 1.0f : 0.0f;
     const int jt0 = (top - 1) / TK;
     float* const part = a.part + ((long)bkv * a.groups + grp) * a.Tpad;
     auto flush = [&](int jt, int par) __attribute__((always_inline)) {
@@ -140,52 +248,21 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
 #pragma unroll
         for (int half = 1; half >= 0; --half) {
             const int base = jt * TK + 32 * half;
-            float w[16];
+            float sum = 0.0f;
+            if (base < u.some && !none_left(stick)) {
+                const f32x16 s = logits<D>(qf, aoff, par * TILE + half * C::SUB);
+                float w[16], mine, all;
+                if (base + 32 > u.all) weights<true>(s, c2, u.sees - base - 16 * hh, hh, w, mine, all);
+                else weights<false>(s, c2, 0, hh, w, mine, all);
+                mine *= stick;
+                stick *= all;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) w[r] = 0.0f;
-            if (base < some && __builtin_amdgcn_ballot_w64(!(carry >= CARRY_EXHAUSTED)) != 0) {
-                f32x16 s;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lds_load16(aoff[i] + par * TILE + 32 * half * ROW)), qf[i], s, 0, 0, 0);
-                const bool mask = base + 32 > all;
-                const int visible = sees - base - 16 * hh;
-                // Eq. 1's product in the lane, from 2^-60 on: w[r] = W_r e_r, W_{r+1} = W_r + w[r]
-                float W = 0x1p-60f;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float e = fast_exp2(s[r] * c2);
-                    if (mask) e = r < visible ? e : 0.0f;
-                    w[r] = W * e;
-                    W += w[r];
-                }
-                float lo, hi;
-                if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(W < 0x1p80f)) == 0, 1)) {
-                    both_halves(fast_log2(W) + 60.0f, lo, hi);
-                    const float kf = fast_exp2(60.0f - (carry + hi + (hh == 0 ? lo : 0.0f)));
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) w[r] *= kf;
-                } else {                       // in the log form
-                    float run = 0.0f;
-#pragma unroll
-                    for (int r = 15; r >= 0; --r) {
-                        const float x = !mask || r < visible ? s[r] * c2 : -INFINITY;
-                        run += sp2(x);
-                        w[r] = x - run;
-                    }
-                    both_halves(run, lo, hi);
-                    const float take = carry + (hh == 0 ? hi : 0.0f);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) w[r] = fast_exp2(w[r] - take);
-                }
-                carry += lo + hi;
+                for (int r = 0; r < 16; ++r) w[r] *= mine;
+                sum = sums_of_lanes(w, n);
             }
-            const float sum = sums_of_lanes(w, n);
             if ((n & 1) == 0) csum[par][wave][32 * half + 16 * hh + key_of_lane(n)] = sum;
         }
-        const int done = __builtin_amdgcn_ballot_w64(!(carry >= CARRY_EXHAUSTED)) == 0 ? -1 : 0;
+        const int done = none_left(stick) ? -1 : 0;
         if (lane == 0) s_done[par][wave] = done;
     }
     if (tid == 0) {
@@ -194,50 +271,212 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     }
 }
 
+// WHAT: 0 the weights of all keys, 1 what a chunk of keys leaves of the sticks, 2 the weights of a chunk
+template <int D, int WHAT>
+__global__ void __launch_bounds__(64 * SNW, 2)
+key_weight_small_kernel(const Args a)
+{
+    using C = Cfg<D>;
+    __shared__ __attribute__((aligned(1024))) char rows[SNW * C::SUB];      // 32 of K a wave
+    __shared__ __attribute__((aligned(1024))) char qrows[C::SUB];
+    __shared__ __attribute__((aligned(16))) float prod[2][SNW][32];         // per round parity: what a wave's keys leave
+    const int unit = a.groups - 1 - (int)blockIdx.x, bkv = blockIdx.y, chunk = WHAT ? blockIdx.z : 0;
+    const int b = bkv / a.Hkv;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 31, hh = lane >> 5;
+    const int len = length_of(a.lens, b, a.T), qlen = length_of(a.qlens, b, a.Tq);
+    const Unit u = unit_of(a, unit, bkv, len - qlen, qlen, n);
+    const int lo = WHAT ? chunk * a.C : 0;
+    const int top = WHAT ? min(u.some, lo + a.C) : u.some;
+    const long at = ((long)bkv * a.groups + unit) * a.chunks + chunk;
+    int* const reach = a.reach + at * 2;
+    float* const left = a.left + at * 32;
+    const bool first = wave == 0 && hh == 0;
+    float stick = u.there ? 1.0f : 0.0f;
+    if (top <= lo) {
+        if (WHAT == 1 && first) left[n] = stick;
+        if (WHAT != 1 && tid == 0) reach[0] = reach[1] = 0;
+        return;
+    }
+    if constexpr (WHAT == 2) {
+        for (int c = a.chunks - 1; c > chunk; --c) stick *= a.left[(at - chunk + c) * 32 + n];
+        if (none_left(stick)) {
+            if (tid == 0) reach[0] = reach[1] = 0;
+            return;
+        }
+    }
+
+    const float c2 = SB_LOG2E / sqrtf((float)D);
+    int off[C::LOADS];
+    sub_offsets<D>(off, lane);
+    const uint16_t* const kg = reinterpret_cast<const uint16_t*>(scalar_base(a.k + (long)bkv * a.Tcap * D));
+    const char* const mine_at = rows + wave * C::SUB;
+    auto fetch = [&](int base) __attribute__((always_inline)) {
+        base = max(base, lo);
+        sub_to_lds<D>(kg + (long)base * D, off, len - 1 - base, mine_at, lane);
+    };
+    // q: every wave some of the loads
+    if (wave < C::LOADS) {
+        const int r = wave * C::BLK_ROWS + lane / C::CPR, r0 = 32 * u.strip;
+        dma16_to_lds_saddr(a.q + (((long)b * a.H + u.head) * a.Tq + r0) * D,
+                           min(r, a.Tq - 1 - r0) * C::ROW + (((lane % C::CPR) ^ swz_perm<D>(r)) << 4), qrows + wave * 1024);
+    }
+    int hi = (top + 31) & ~31;
+    fetch(hi - 32 * (wave + 1));
+    uint32_t aoff[D / 16];
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) aoff[s] = lds_offset(mine_at) + tile_off_perm<D>(perm_row(n), 2 * s + hh);
+    dma_wait<C::LOADS>();
+    barrier_lds();
+    bf16x8 qf[D / 16];
+    read_q<D>(qf, lds_offset(qrows), n, hh, u.there);
+
+    float* const part = a.part + ((long)bkv * a.groups + unit) * a.Tpad;
+    const int hi0 = hi;
+    for (int par = 0; hi > lo; hi -= 32 * SNW, par ^= 1) {
+        const int base = hi - 32 * (wave + 1);
+        dma_wait<0>();
+        const f32x16 s = logits<D>(qf, aoff, 0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the rows have been read)
+        if (hi - 32 * SNW > lo) fetch(base - 32 * SNW);
+        float w[16], mine = 0.0f, all = 1.0f;
+        if (base >= lo) {
+            if (base + 32 > u.all) weights<true>(s, c2, u.sees - base - 16 * hh, hh, w, mine, all);
+            else weights<false>(s, c2, 0, hh, w, mine, all);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) w[r] = 0.0f;
+        }
+        if (hh == 0) prod[par][wave][n] = all;
+        barrier_lds();
+        float before = stick;
+#pragma unroll
+        for (int j = 0; j < SNW; ++j) {
+            const float p = prod[par][j][n];
+            if (j < wave) before *= p;
+            stick *= p;
+        }
+        if constexpr (WHAT != 1) {
+            if (base >= lo) {
+                mine *= before;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) w[r] *= mine;
+                const float sum = sums_of_lanes(w, n);
+                if ((n & 1) == 0) part[base + 16 * hh + key_of_lane(n)] = sum;
+            }
+        }
+        if (none_left(stick)) {
+            hi -= 32 * SNW;
+            break;
+        }
+    }
+    if (WHAT == 1 && first) left[n] = stick;
+    if (WHAT != 1 && tid == 0) {
+        reach[0] = max(hi, lo);
+        reach[1] = hi0;
+    }
+    dma_wait<0>();                             // (rows asked for before the end was known)
+}
+
+// Groups by wave in turn, 64 keys a workgroup: a wave asks for four groups' numbers at a time, and how far a group reaches is the same for all its lanes.
 __global__ void __launch_bounds__(SUM_THREADS)
 key_weight_sum_kernel(const Args a)
 {
-    const int bkv = blockIdx.y, key = blockIdx.x * SUM_THREADS + threadIdx.x;
+    constexpr int WAVES = SUM_THREADS / 64, DEEP = 4;
+    __shared__ float sums[WAVES][64];
+    const int bkv = blockIdx.y, lane = threadIdx.x & 63, key = blockIdx.x * 64 + lane;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int len = length_of(a.lens, bkv / a.Hkv, a.T);
-    if (blockIdx.x * SUM_THREADS >= len) return;
-    const float* part = a.part + (long)bkv * a.groups * a.Tpad;
-    const int* reach = a.reach + (long)bkv * a.groups * 2;
+    if ((int)blockIdx.x * 64 >= len) return;
+    const float* part = a.part + (long)bkv * a.groups * a.Tpad + key;
+    const int2* reach = reinterpret_cast<const int2*>(a.reach) + (long)bkv * a.groups * a.chunks + blockIdx.x * 64 / a.C;
     float s = 0.0f;
-    for (int g = 0; g < a.groups; ++g) {
-        const int lo = reach[2 * g], hi = reach[2 * g + 1];
-        if (key >= lo && key < hi) s += part[(long)g * a.Tpad + key];
+    for (int g0 = wave; g0 < a.groups; g0 += DEEP * WAVES) {
+        int2 r[DEEP];
+        float x[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) r[i] = reach[(long)min(g0 + i * WAVES, a.groups - 1) * a.chunks];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            x[i] = 0.0f;
+            if (g0 + i * WAVES < a.groups && key >= r[i].x && key < r[i].y) x[i] = part[(long)(g0 + i * WAVES) * a.Tpad];
+        }
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) s += x[i];
     }
-    if (key < len) {
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && key < len) {
+        s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) s += sums[w][lane];
         const long at = (long)bkv * a.Tcap + key;
         a.score_out[at] = (a.score ? a.score[at] : 0.0f) + s;
     }
 }
 
-int groups_of(int H, int Hkv, int Tq) { return (int)(((long)((Tq + 31) / 32) * (H / Hkv) + NW - 1) / NW); }
-int pad_of(int T) { return (T + TK - 1) / TK * TK; }
+struct Plan {
+    bool small;
+    int groups, chunks, C;
+    int Tpad;
+    size_t floats(int BHkv) const { return (size_t)BHkv * groups * ((size_t)Tpad + (size_t)chunks * (2 + (chunks > 1 ? 32 : 0))); }
+};
+Plan plan_of(int B, int H, int Hkv, int Tq, int T)
+{
+    const int G = H / Hkv, units = (Tq + 31) / 32 * G, Tpad = (T + TK - 1) / TK * TK;
+    const long all = (long)B * Hkv * units;
+    Plan p = {all <= 1024, 0, 1, Tpad, Tpad};
+    p.groups = p.small ? units : (units + NW - 1) / NW;
+    if (p.small) {
+        constexpr int round = 32 * SNW;
+        const int rounds = (T + round - 1) / round;
+        const int want = (int)std::max(1L, std::min<long>(rounds / 2, 1024 / all));
+        if (want > 1) {
+            p.C = (rounds + want - 1) / want * round;
+            p.chunks = (T + p.C - 1) / p.C;
+        }
+        if (p.chunks == 1) p.C = Tpad;
+    }
+    return p;
+}
+
+template <int D> hipError_t launch_d(const Args& a, const Plan& p, int BHkv, hipStream_t stream)
+{
+    if (!p.small)
+        return launch_workgroups((long)BHkv * a.groups, 64 * NW, [&](unsigned wgs, int first) {
+            hipLaunchKernelGGL((key_weight_kernel<D>), dim3(wgs), dim3(64 * NW), 0, stream, a, BHkv, first);
+        });
+    const dim3 grid((unsigned)a.groups, (unsigned)BHkv, (unsigned)a.chunks), threads(64 * SNW);
+    if (a.chunks == 1) {
+        hipLaunchKernelGGL((key_weight_small_kernel<D, 0>), grid, threads, 0, stream, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((key_weight_small_kernel<D, 1>), grid, threads, 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((key_weight_small_kernel<D, 2>), grid, threads, 0, stream, a);
+    return hipGetLastError();
+}
 
 }  // namespace
 
 size_t key_weight_workspace_bytes(int B, int H, int Hkv, int Tq, int T)
 {
-    return sizeof(float) * (size_t)B * Hkv * groups_of(H, Hkv, Tq) * ((size_t)pad_of(T) + 2);
+    return sizeof(float) * plan_of(B, H, Hkv, Tq, T).floats(B * Hkv);
 }
 
 hipError_t launch_key_weight(const uint16_t* q, const uint16_t* k, const int* lens, const int* qlens, const float* score, float* score_out,
                              float* workspace, int B, int H, int Hkv, int Tq, int T, int Tcap, int d, hipStream_t stream)
 {
-    Args a = {q, k, lens, qlens, score, score_out, workspace, nullptr, H, Hkv, H / Hkv, Tq, T, Tcap, pad_of(T), groups_of(H, Hkv, Tq)};
-    a.reach = reinterpret_cast<int*>(workspace + (size_t)B * Hkv * a.groups * a.Tpad);
+    const Plan p = plan_of(B, H, Hkv, Tq, T);
     const int BHkv = B * Hkv;
-    auto go = [&](unsigned wgs, int first) {
-        const dim3 grid(wgs), threads(64 * NW);
-        if (d == 32) hipLaunchKernelGGL((key_weight_kernel<32>), grid, threads, 0, stream, a, BHkv, first);
-        else if (d == 64) hipLaunchKernelGGL((key_weight_kernel<64>), grid, threads, 0, stream, a, BHkv, first);
-        else hipLaunchKernelGGL((key_weight_kernel<128>), grid, threads, 0, stream, a, BHkv, first);
-    };
-    const hipError_t e = launch_workgroups((long)BHkv * a.groups, 64 * NW, go);
+    Args a = {q, k, lens, qlens, score, score_out, workspace, nullptr, nullptr, H, Hkv, H / Hkv, Tq, T, Tcap, p.Tpad, p.groups, p.chunks, p.C};
+    a.left = workspace + (size_t)BHkv * p.groups * p.Tpad;
+    a.reach = reinterpret_cast<int*>(a.left + (p.chunks > 1 ? (size_t)BHkv * p.groups * p.chunks * 32 : 0));
+    const hipError_t e = d == 32 ? launch_d<32>(a, p, BHkv, stream) : d == 64 ? launch_d<64>(a, p, BHkv, stream) : launch_d<128>(a, p, BHkv, stream);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(key_weight_sum_kernel, dim3((unsigned)((T + SUM_THREADS - 1) / SUM_THREADS), (unsigned)BHkv), dim3(SUM_THREADS), 0, stream, a);
+    hipLaunchKernelGGL(key_weight_sum_kernel, dim3((unsigned)((T + 63) / 64), (unsigned)BHkv), dim3(SUM_THREADS), 0, stream, a);
     return hipGetLastError();
 }
 
