@@ -10,14 +10,19 @@
 //   combine launch   a workgroup per query head adds the chunks up in a fixed order; with scores, one per (kv head, chunk)
 //                    shifts the weights of its keys, sums them over the group's heads and adds the score
 //
-// A workgroup takes its keys from the nearest down in rounds of 32 per wave, wave 0 the nearest.
+// A workgroup takes its keys from the nearest down in rounds of R tiles of 32 per wave, wave 0 the nearest.
 //   logits   z[key][head] = K q: 16x16x32 bf16 MFMA, A = 16 rows of K, B = the query heads of the group.  A lane loads the D / 8
 //            bytes of its row that make up one A operand after the other (the order of the columns is free as long as q comes in
-//            the same one), and converts them in registers, the scale with them.
-//   weights  where the MFMA leaves the logits: a lane has four consecutive keys of one head, twice; the chain of Eq. 1's product
-//            over the four, their logarithm across the four lanes and the eight waves of a head (by LDS, one barrier a round).
+//            the same one), and converts them in registers, the scale with them.  Rows go to the MFMAs so that a lane gets eight
+//            consecutive keys of a head.
+//   weights  where the MFMA leaves the logits: Eq. 1's product over the lane's eight keys, then across the four lanes of a tile,
+//            the tiles and the waves (by LDS, one barrier a round).  What is left of the stick is carried as it is, not by its
+//            logarithm: the keys' scores are results in fp32.  From less than 2^-126 of it on, weights are subnormal at most and count as zero.
 //   output   O^T[c][head] += V^T w: a lane's eight weights are the B operand as they lie; it loads D / 16 columns of those same
 //            eight rows of V, converts, and an in-register transposition (one v_perm per packed pair) makes the A operands.
+// The 16 columns of the MFMAs are more than most groups have heads.  Their copies of a head take a tile each (R of them), which
+// divides the vector instructions of the weights by R, and the upper 8 bits of a weight or the 8 below (o gets 16 bits of a weight; o itself has
+// 8), which halves the MFMAs of the output; the columns of a head are added up at the end.
 #include "sb_kernels.h"
 #include "sb_kv4.h"
 #include "sb_mma.h"
@@ -26,9 +31,10 @@ namespace sb {
 namespace {
 
 constexpr int GMAX = 16;               // query heads of a group per workgroup: the columns of the MFMA
-constexpr int KW = 32;                 // keys per wave and round
+constexpr int KW = 32;                 // keys of a tile
 constexpr int NEAR_NW = 8, FAR_NW = 4;
 constexpr int NEAR = KW * NEAR_NW;     // keys of a near launch that has a far one behind it
+constexpr float LEAST = 0x1p-126f;     // of the stick
 constexpr int ALONE = 2048;            // a cache is the near launch's alone up to here
 constexpr int MAXSLOT = 128;           // chunks, the nearest keys among them: two per lane of a wave
 constexpr long FAR_WGS = 4096;         // workgroups of the far launch, all heads together
@@ -44,9 +50,10 @@ struct Args {
     float* score_out;                  // nullptr: not wanted
     uint16_t* o;
     float* m;
-    float *part_o, *part_a;            // [heads][slots][D], [heads][slots]: slot 0 the nearest
+    float *part_o, *part_a, *part_l;   // [heads][slots][D], [heads][slots]: slot 0 the nearest; share of the stick that it leaves, and -log2 of that where m is wanted
     float* wl;                         // [heads][Tcap]: weights inside their chunk, where scores are combined
     int T, Tcap, Hkv, G, near, C, slots;
+    int lg;                            // log2 of the columns that a copy of the heads takes
 };
 
 __device__ __forceinline__ int length_of(const Args& a, int b)
@@ -75,22 +82,21 @@ __device__ __forceinline__ float wave_sum(float x)
     return a + b;
 }
 
-// sum over the lanes below this one, and over all in `total`
-template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_or_zero(float x)
+// product over the lanes below this one, and over all in `total`
+template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_or_one(float x)
 {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false));
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0x3f800000, __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false));
 }
 __device__ __forceinline__ float wave_prefix(float v, float& total)
 {
-    float inc = v;
-    inc += dpp_or_zero<0x111, 0xF>(inc);                  // row_shr:1, 2, 4, 8
-    inc += dpp_or_zero<0x112, 0xF>(inc);
-    inc += dpp_or_zero<0x114, 0xF>(inc);
-    inc += dpp_or_zero<0x118, 0xF>(inc);
-    inc += dpp_or_zero<0x142, 0xA>(inc);                  // row_bcast:15 into rows 1 and 3
-    inc += dpp_or_zero<0x143, 0xC>(inc);                  // row_bcast:31 into rows 2 and 3
-    total = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inc), 63));
-    return inc - v;
+    v *= dpp_or_one<0x111, 0xF>(v);                       // row_shr:1, 2, 4, 8
+    v *= dpp_or_one<0x112, 0xF>(v);
+    v *= dpp_or_one<0x114, 0xF>(v);
+    v *= dpp_or_one<0x118, 0xF>(v);
+    v *= dpp_or_one<0x142, 0xA>(v);                       // row_bcast:15 into rows 1 and 3
+    v *= dpp_or_one<0x143, 0xC>(v);                       // row_bcast:31 into rows 2 and 3
+    total = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+    return dpp_or_one<0x138, 0xF>(v);                     // wave_shr:1
 }
 
 // `even`: v of this lane's column in row 0 (lanes 0 .. 31) or 2 (32 .. 63), `odd`: in row 1 or 3
@@ -101,13 +107,14 @@ __device__ __forceinline__ void both_rows(float v, float& even, float& odd)
     odd = __builtin_bit_cast(float, (int)sw[1]);
 }
 
-// what a lane loads of 32 keys
-template <int D> struct Tile {
-    typedef __attribute__((ext_vector_type(4))) uint32_t u4;
-    uint32_t k[2][D / 32];             // row l16 (+ 16): columns lq D / 4 .. + D / 4 - 1
-    uint32_t ks[2];                    // and their scale
-    uint32_t v[8];                     // rows 16 (i / 4) + 4 lq + i % 4: columns D / 16 l16 .. + D / 16 - 1
-    uint32_t vs[2][D / 32];            // scales of four rows each, bytes as they lie
+// what a lane loads of a tile
+template <int D> struct KTile {
+    uint32_t k[2][D / 32];             // rows 8 (l16 / 4) + 4 h + l16 % 4: columns lq D / 4 .. + D / 4 - 1
+    uint32_t s[2];                     // and their scale
+};
+template <int D> struct VTile {
+    uint32_t v[8];                     // rows 8 lq + i: columns D / 16 l16 .. + D / 16 - 1
+    uint32_t s[D / 16];                // scales of the eight rows, bytes as they lie
 };
 
 template <class V> __device__ __forceinline__ V load_as(const uint8_t* p)
@@ -116,71 +123,69 @@ template <class V> __device__ __forceinline__ V load_as(const uint8_t* p)
     __builtin_memcpy(&x, p, sizeof(V));
     return x;
 }
+// N words from p on
+template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p)
+{
+    if constexpr (N == 1) {
+        w[0] = load_as<uint32_t>(p);
+    } else if constexpr (N == 2) {
+        const uint2 x = load_as<uint2>(p);
+        w[0] = x.x;
+        w[1] = x.y;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+            const u32x4 x = load_as<u32x4>(p + 4 * j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[j + i] = x[i];
+        }
+    }
+}
 
-template <int D> __device__ __forceinline__ void fetch(Tile<D>& t, const uint8_t* kc, const uint8_t* ks, const uint8_t* vc, const uint8_t* vs,
-                                                       int base, int l16, int lq)
+template <int D> __device__ __forceinline__ void fetch_k(KTile<D>& t, const uint8_t* kc, const uint8_t* ks, int base, int l16, int lq)
 {
     constexpr int ROW = D / 2, SROW = D / KV4_BLOCK;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int row = base + 16 * h + l16;
-        const uint8_t* p = kc + (long)row * ROW + lq * (ROW / 4);
-        if constexpr (D == 128) {
-            const u32x4 x = load_as<u32x4>(p);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t.k[h][i] = x[i];
-        } else if constexpr (D == 64) {
-            const uint2 x = load_as<uint2>(p);
-            t.k[h][0] = x.x;
-            t.k[h][1] = x.y;
-        } else {
-            t.k[h][0] = load_as<uint32_t>(p);
-        }
-        t.ks[h] = ks[(long)row * SROW + lq * SROW / 4];
+        const int row = base + 8 * (l16 >> 2) + 4 * h + (l16 & 3);
+        load_words(t.k[h], kc + (long)row * ROW + lq * (ROW / 4));
+        t.s[h] = ks[(long)row * SROW + lq * SROW / 4];
     }
+}
+template <int D> __device__ __forceinline__ void fetch_v(VTile<D>& t, const uint8_t* vc, const uint8_t* vs, int base, int l16, int lq)
+{
+    constexpr int ROW = D / 2, SROW = D / KV4_BLOCK;
+    const long row = base + 8 * lq;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint8_t* p = vc + (long)(base + 16 * (i / 4) + 4 * lq + i % 4) * ROW + l16 * (ROW / 16);
+        const uint8_t* p = vc + (row + i) * ROW + l16 * (ROW / 16);
         t.v[i] = D == 128 ? load_as<uint32_t>(p) : D == 64 ? load_as<uint16_t>(p) : *p;
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint8_t* p = vs + (long)(base + 16 * h + 4 * lq) * SROW;
-        if constexpr (D == 128) {
-            const u32x4 x = load_as<u32x4>(p);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t.vs[h][i] = x[i];
-        } else if constexpr (D == 64) {
-            const uint2 x = load_as<uint2>(p);
-            t.vs[h][0] = x.x;
-            t.vs[h][1] = x.y;
-        } else {
-            t.vs[h][0] = load_as<uint32_t>(p);
-        }
-    }
+    load_words(t.s, vs + row * SROW);
 }
 
-// scale of row i of the eight, of this lane's columns (exponent bits; what stands below them does not count)
-template <int D> __device__ __forceinline__ uint32_t v_scale(const Tile<D>& t, int i, int l16)
+// scale of row i, of this lane's columns (exponent bits; what stands below them does not count)
+template <int D> __device__ __forceinline__ uint32_t v_scale(const VTile<D>& t, int i, int l16)
 {
     constexpr int PER = 128 / D;       // rows in a word
-    const int r = i % 4;
-    const uint32_t w = t.vs[i / 4][r / PER];
-    // byte of the row's first block: r % PER * D / 32; of this lane's block: + l16 D / 16 / 32
-    const int sh = 24 - 8 * ((r % PER) * (D / KV4_BLOCK)) - 8 * (l16 * (D / 16) / KV4_BLOCK);
-    return (w << sh) >> 1;
+    // byte of the row's first block: i % PER * D / 32; of this lane's block: + l16 D / 16 / 32
+    const int sh = 24 - 8 * ((i % PER) * (D / KV4_BLOCK)) - 8 * (l16 * (D / 16) / KV4_BLOCK);
+    return (t.s[i / PER] << sh) >> 1;
 }
 
-template <int D, bool FAR>
+// R: tiles of a wave and round.  PIECES: the columns' copies take a weight's upper and lower bits; without, two MFMAs do
+template <int D, bool FAR, int R, bool PIECES>
 __global__ void __launch_bounds__(64 * (FAR ? FAR_NW : NEAR_NW), 2)
 decode_kv4_kernel(const Args a)
 {
     constexpr int NW = FAR ? FAR_NW : NEAR_NW;
     constexpr int NTHR = 64 * NW;
-    constexpr int KEYS = KW * NW;          // keys per round
+    constexpr int NT = NW * R;             // tiles of a round
+    constexpr int KEYS = KW * NT;
     constexpr int CW = D / 16;             // columns of V per lane
     constexpr int CH = D / 4;              // 16-byte chunks of a head's columns
-    __shared__ __attribute__((aligned(16))) float tot[2][GMAX][NW];      // per round parity: sp2 over a wave's keys
+    __shared__ __attribute__((aligned(16))) float tot[2][GMAX][NT];      // per round parity: what a tile leaves of the stick
+    __shared__ float s_log[NW][GMAX];
     __shared__ __attribute__((aligned(16))) f32x4 ored[NW * GMAX * CH];
 
     const int bkv = FAR ? blockIdx.y : blockIdx.x;     // entry * Hkv + kv head
@@ -195,12 +200,17 @@ decode_kv4_kernel(const Args a)
     const int lo = max(0, FAR ? top - a.C : top - a.near);
     const long hq0 = (long)bkv * a.G + g0;
     const int live = min(GMAX, a.G - g0);
-    const long head = hq0 + min(l16, live - 1);
+    // this lane's column: head l16 % 2^lg, copy l16 / 2^lg
+    const int hc = l16 & ((1 << a.lg) - 1), copy = l16 >> a.lg;
+    const int mytile = R == 1 ? 0 : copy & (R - 1);
+    const bool lower = PIECES && (copy / R & 1);
+    const bool first = copy < R && hc < live;          // one column for each tile and head
+    const long head = hq0 + min(hc, live - 1);
     const float c2 = SB_LOG2E / sqrtf((float)D);
 
     if constexpr (FAR) {
         if (top <= 0) return;
-        if (!a.m && a.near > 0 && __builtin_amdgcn_ballot_w64(!(a.part_a[head * a.slots] >= CARRY_EXHAUSTED)) == 0) return;
+        if (!a.m && a.near > 0 && __builtin_amdgcn_ballot_w64(!(a.part_a[head * a.slots] < LEAST)) == 0) return;
     }
 
     const uint8_t* const kc = a.kc + (long)bkv * a.Tcap * (D / 2);
@@ -208,170 +218,180 @@ decode_kv4_kernel(const Args a)
     const uint8_t* const ks = a.ks + (long)bkv * a.Tcap * (D / KV4_BLOCK);
     const uint8_t* const vs = a.vs + (long)bkv * a.Tcap * (D / KV4_BLOCK);
 
-    bf16x8 qw[D / 32];                     // B operand: head l16 (columns past `live` repeat the last one)
+    bf16x8 qw[D / 32];                     // B operand
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) qw[s] = *reinterpret_cast<const bf16x8*>(a.q + head * D + lq * (D / 4) + 8 * s);
 
-    f32x4 acc[CW];                         // O^T: row 4 lq + r of MFMA e is column CW (4 lq + r) + e, head l16
+    f32x4 acc[CW];                         // O^T: row 4 lq + r of MFMA e is column CW (4 lq + r) + e, column l16
 #pragma unroll
     for (int e = 0; e < CW; ++e) acc[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    float carry = 0.0f;                    // sp2 of the keys already passed, head l16
-    const float odd_counts = (lq & 1) ? 0.0f : 1.0f, upper_counts = lq < 2 ? 1.0f : 0.0f;
+    float stick = 1.0f, logs = 0.0f;       // left by the keys already passed; -log2 of what this lane's own keys left
     int par = 0, hi = top;
+    KTile<D> kt[R];
+    VTile<D> vt[R];
+    // tile j of this wave; where that is below lo there is none, and the last one is loaded
+    auto base_of = [&](int j) __attribute__((always_inline)) { return hi - KW * (wave * R + j + 1); };
+    auto valid_of = [&](int j) __attribute__((always_inline)) { return base_of(j) < lo ? 0 : len - base_of(j); };
 
-    // one round on the keys in t; whether another follows.  n: the next one's
-    auto round = [&](Tile<D>& t, Tile<D>& n) __attribute__((always_inline)) {
-        const int base = hi - KW * (wave + 1);             // this wave's keys; where that is below lo it has none, and loads the last ones
-        const int valid = base < lo ? 0 : len - base;
+    // one round; whether another follows
+    auto round = [&]() __attribute__((always_inline)) {
         const bool more = hi - KEYS > lo;
-        if (more) fetch<D>(n, kc, ks, vc, vs, max(base - KEYS, lo), l16, lq);
-        // ---- logits, in base 2
-        f32x4 x[2];
+        // ---- logits of the lane's eight keys, in base 2
+        float x[8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
-            const uint32_t s = t.ks[h] << 23;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                const uint32_t w = t.k[h][i];
-                const u32x4 p = {kv4_pair<0>(w, s), kv4_pair<1>(w, s), kv4_pair<2>(w, s), kv4_pair<3>(w, s)};
-                z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p), qw[i], z, 0, 0, 0);
-            }
-            x[h] = z * c2;
-        }
-        if (valid < KW) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (16 * h + 4 * lq + r >= valid) x[h][r] = -INFINITY;
-        }
-        // ---- the lane's chains: w[r] = e_r prod_{r' < r} (1 + e_r'), l = log2 of the whole product
-        float w[2][4], l[2];
-        float most = 0.0f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float W = 1.0f;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                w[h][r] = W * fast_exp2(x[h][r]);
-                W += w[h][r];
-            }
-            l[h] = fast_log2(W);
-            most += W;
-        }
-        // where a product overflows, w is the logarithm of the weight inside the lane
-        const bool logs = __builtin_amdgcn_ballot_w64(!(most < INFINITY)) != 0;
-        if (__builtin_expect(logs, 0)) {
+        for (int j = 0; j < R; ++j) {
+            const int valid = valid_of(j);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                l[h] = 0.0f;
+                f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+                const uint32_t s = kt[j].s[h] << 23;
 #pragma unroll
-                for (int r = 3; r >= 0; --r) {
-                    l[h] += sp2(x[h][r]);
-                    w[h][r] = x[h][r] - l[h];
+                for (int i = 0; i < D / 32; ++i) {
+                    const uint32_t w = kt[j].k[h][i];
+                    const u32x4 p = {kv4_pair<0>(w, s), kv4_pair<1>(w, s), kv4_pair<2>(w, s), kv4_pair<3>(w, s)};
+                    z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p), qw[i], z, 0, 0, 0);
                 }
+                if (valid < KW)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[r] = 8 * lq + 4 * h + r < valid ? z[r] : -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[4 * h + r] = j == 0 || mytile == j ? z[r] : x[4 * h + r];
             }
         }
-        // ---- across the lanes of a head: the row above of a pair, and the upper half, are nearer
-        float behind[2], sum[2];
+        if (more) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float even, odd, lower, upper;
-            both_rows(l[h], even, odd);
-            both_halves(even + odd, lower, upper);
-            sum[h] = lower + upper;
-            behind[h] = __builtin_fmaf(odd, odd_counts, upper * upper_counts);
+            for (int j = 0; j < R; ++j) fetch_k<D>(kt[j], kc, ks, max(base_of(j) - KEYS, lo), l16, lq);
         }
-        if (lq == 0) tot[par][l16][wave] = sum[0] + sum[1];
-        barrier_lds();
-        float above = carry;
+        // ---- the lane's chain: w[i] = e_i prod_{i' < i} (1 + e_i'), e = sigma / (1 - sigma); norm makes it the weight where the stick is whole
+        // before the lane's nearest key, `leave` is what the eight keys leave
+        float w[8], norm, leave;
+        float W = 1.0f;
 #pragma unroll
-        for (int j = 0; j < NW; j += 4) {
-            const f32x4 s = *reinterpret_cast<const f32x4*>(&tot[par][l16][j]);
+        for (int i = 0; i < 8; ++i) {
+            x[i] *= c2;
+            w[i] = W * fast_exp2(x[i]);
+            W += w[i];
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(W < 0x1p120f)) == 0, 1)) {
+            norm = leave = __builtin_amdgcn_rcpf(W);
+            if (a.m) logs += fast_log2(W);
+        } else {                           // in the log form
+            float run = 0.0f;
+#pragma unroll
+            for (int i = 7; i >= 0; --i) {
+                run += sp2(x[i]);
+                w[i] = fast_exp2(x[i] - run);
+            }
+            norm = 1.0f;
+            leave = fast_exp2(-run);
+            logs += run;
+        }
+        // ---- across the four lanes of a tile (the odd one of a pair and the upper half are nearer), the tiles and waves
+        float even, odd, lowhalf, upphalf;
+        both_rows(leave, even, odd);
+        both_halves(even * odd, lowhalf, upphalf);
+        norm *= ((lq & 1) ? 1.0f : odd) * (lq < 2 ? upphalf : 1.0f);
+        if (lq == 0 && first) tot[par][hc][wave * R + mytile] = lowhalf * upphalf;
+        barrier_lds();
+        float before = stick;
+        const int mine = wave * R + mytile;
+#pragma unroll
+        for (int j = 0; j < NT; j += 4) {
+            const f32x4 p = *reinterpret_cast<const f32x4*>(&tot[par][min(hc, live - 1)][j]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (j + i < wave) above += s[i];
-                carry += s[i];
+                before *= j + i < mine ? p[i] : 1.0f;
+                stick *= p[i];
             }
         }
-        // ---- weights
+        norm *= before;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float take = above + behind[h] + (h == 0 ? sum[1] : 0.0f);
-            if (__builtin_expect(logs, 0)) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) w[h][r] = fast_exp2(w[h][r] - take);
-            } else {
-                const float kf = fast_exp2(-(take + l[h]));
-#pragma unroll
-                for (int r = 0; r < 4; ++r) w[h][r] *= kf;
-            }
-        }
-        if (a.score_out && base >= lo) {
+        for (int i = 0; i < 8; ++i) w[i] *= norm;
+        if (a.score_out) {
+            const int base = hi - KW * (mine + 1);
             if (a.wl) {
-                if (l16 < live)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        *reinterpret_cast<f32x4*>(a.wl + (hq0 + l16) * a.Tcap + base + 16 * h + 4 * lq) = f32x4{w[h][0], w[h][1], w[h][2], w[h][3]};
-            } else {
+                if (first && base >= lo) {
+                    float* p = a.wl + (hq0 + hc) * a.Tcap + base + 8 * lq;
+                    *reinterpret_cast<f32x4*>(p) = f32x4{w[0], w[1], w[2], w[3]};
+                    *reinterpret_cast<f32x4*>(p + 4) = f32x4{w[4], w[5], w[6], w[7]};
+                }
+            } else if constexpr (!FAR) {   // (R = 1)
                 f32x4 s[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[h][r] = row_sum(l16 < live ? w[h][r] : 0.0f);
-                if (l16 < 2) {
-                    const int key = base + 16 * l16 + 4 * lq;
+                for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = row_sum(first ? w[i] : 0.0f);
+                if (l16 < 2 && base >= lo) {
+                    const int key = base + 8 * lq + 4 * l16;
                     const long at = (long)bkv * a.Tcap + key;
-                    const f32x4 mine = l16 ? s[1] : s[0];
+                    const f32x4 own = l16 ? s[1] : s[0];
                     if (key + 4 <= len) {
                         const f32x4 was = a.score ? *reinterpret_cast<const f32x4*>(a.score + at) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                        *reinterpret_cast<f32x4*>(a.score_out + at) = was + mine;
+                        *reinterpret_cast<f32x4*>(a.score_out + at) = was + own;
                     } else {
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (key + r < len) a.score_out[at + r] = (a.score ? a.score[at + r] : 0.0f) + mine[r];
+                            if (key + r < len) a.score_out[at + r] = (a.score ? a.score[at + r] : 0.0f) + own[r];
                     }
                 }
             }
         }
-        // ---- output.  Weights as two bf16 (16 bits of mantissa): o itself is rounded to eight
+        // ---- output
         bf16x8 w0, w1;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            w0[i] = (__bf16)w[i / 4][i % 4];
-            w1[i] = (__bf16)(w[i / 4][i % 4] - (float)w0[i]);
+            w0[i] = (__bf16)w[i];
+            const float rest = w[i] - (float)w0[i];
+            if (PIECES) w0[i] = (__bf16)(lower ? rest : w[i]);
+            else w1[i] = (__bf16)rest;
         }
-        uint32_t pv[8][(CW + 1) / 2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint32_t s = v_scale<D>(t, i, l16);
-            if (valid < KW && 16 * (i / 4) + 4 * lq + i % 4 >= valid) s = 0x3f800000u;      // (whatever lies there, a zero weight makes it zero)
-            pv[i][0] = kv4_pair<0>(t.v[i], s);
-            if constexpr (CW >= 4) pv[i][1] = kv4_pair<1>(t.v[i], s);
-            if constexpr (CW >= 8) {
-                pv[i][2] = kv4_pair<2>(t.v[i], s);
-                pv[i][3] = kv4_pair<3>(t.v[i], s);
+        for (int j = 0; j < R; ++j) {
+            const int valid = valid_of(j);
+            bf16x8 wb = w0;
+            if (R > 1) {
+                u32x4 y = __builtin_bit_cast(u32x4, w0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = mytile == j ? y[i] : 0u;
+                wb = __builtin_bit_cast(bf16x8, y);
+            }
+            uint32_t pv[8][CW / 2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t s = v_scale<D>(vt[j], i, l16);
+                if (valid < KW && 8 * lq + i >= valid) s = 0x3f800000u;        // (whatever lies there, a zero weight makes it zero)
+                const uint32_t v = vt[j].v[i];
+                pv[i][0] = kv4_pair<0>(v, s);
+                if constexpr (CW >= 4) pv[i][1] = kv4_pair<1>(v, s);
+                if constexpr (CW >= 8) {
+                    pv[i][2] = kv4_pair<2>(v, s);
+                    pv[i][3] = kv4_pair<3>(v, s);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < CW; ++e) {
+                u32x4 y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    y[i] = __builtin_amdgcn_perm(pv[2 * i + 1][e >> 1], pv[2 * i][e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
+                const bf16x8 av = __builtin_bit_cast(bf16x8, y);
+                if (!PIECES) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, w1, acc[e], 0, 0, 0);
+                acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, wb, acc[e], 0, 0, 0);
             }
         }
+        if (more) {
 #pragma unroll
-        for (int e = 0; e < CW; ++e) {
-            u32x4 y;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                y[i] = __builtin_amdgcn_perm(pv[2 * i + 1][e >> 1], pv[2 * i][e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
-            const bf16x8 av = __builtin_bit_cast(bf16x8, y);
-            acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, w1, acc[e], 0, 0, 0);
-            acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, w0, acc[e], 0, 0, 0);
+            for (int j = 0; j < R; ++j) fetch_v<D>(vt[j], vc, vs, max(base_of(j) - KEYS, lo), l16, lq);
         }
         hi -= KEYS;
         par ^= 1;
-        return more && (FAR || a.m || __builtin_amdgcn_ballot_w64(!(carry >= CARRY_EXHAUSTED)) != 0);
+        return more && (FAR || a.m || __builtin_amdgcn_ballot_w64(!(stick < LEAST)) != 0);
     };
     if (hi > lo) {
-        Tile<D> ta, tb;
-        fetch<D>(ta, kc, ks, vc, vs, max(hi - KW * (wave + 1), lo), l16, lq);
-        while (round(ta, tb) && round(tb, ta)) {}
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            fetch_k<D>(kt[j], kc, ks, max(base_of(j), lo), l16, lq);
+            fetch_v<D>(vt[j], vc, vs, max(base_of(j), lo), l16, lq);
+        }
+        while (round()) {}
     }
     // keys that no stick was left for keep their scores
     if (!FAR && a.score_out && !a.wl && a.score_out != a.score)
@@ -380,9 +400,9 @@ decode_kv4_kernel(const Args a)
         for (int g = 0; g < live; ++g)
             for (int i = lo + tid; i < hi; i += NTHR) a.wl[(hq0 + g) * a.Tcap + i] = 0.0f;
 
-    // ---- the waves' shares: a lane holds 4 CW columns of its head, CW chunks of 16 bytes, their places xor-ed with the head
-    if (l16 < live) {
-        f32x4* const r = ored + (wave * live + l16) * CH;
+    // ---- the columns' and waves' shares: a lane holds 4 CW columns of V of its column, CW chunks of 16 bytes, their places xor-ed with the column
+    {
+        f32x4* const r = ored + (wave * GMAX + l16) * CH;
 #pragma unroll
         for (int j = 0; j < CW; ++j) {
             f32x4 y;
@@ -390,30 +410,48 @@ decode_kv4_kernel(const Args a)
             for (int i = 0; i < 4; ++i) y[i] = acc[(4 * j + i) % CW][(4 * j + i) / CW];
             r[(CW * lq + j) ^ (l16 & 7)] = y;
         }
-        if (wave == 0 && lq == 0) tot[par][l16][0] = carry;
+    }
+    if (wave == 0 && lq == 0 && first && mytile == 0) tot[par][hc][0] = stick;
+    if (a.m) {
+        float even, odd, lowhalf, upphalf;
+        both_rows(logs, even, odd);
+        both_halves(even + odd, lowhalf, upphalf);
+        if (lq == 0) s_log[wave][l16] = lowhalf + upphalf;
     }
     barrier_lds();
+    constexpr int COPIES = R * (PIECES ? 2 : 1);           // columns of a head
     for (int i = tid; i < live * CH; i += NTHR) {
         const int g = i / CH, c = i % CH;
         f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < NW; ++w) s += ored[(w * live + g) * CH + (c ^ (g & 7))];
-        const float total = tot[par][g][0];
+        for (int w = 0; w < NW; ++w)
+#pragma unroll
+            for (int k = 0; k < COPIES; ++k) {
+                const int col = g + (k << a.lg);
+                s += ored[(w * GMAX + col) * CH + (c ^ (col & 7))];
+            }
+        const float left = tot[par][g][0];
+        float log = 0.0f;
+        if (a.m && c == 0)
+            for (int w = 0; w < NW; ++w)
+                for (int k = 0; k < R; ++k) log += s_log[w][g + (k << a.lg)];
         const long h = hq0 + g;
-        if (!FAR && (a.slots == 1 || (!a.m && total >= CARRY_EXHAUSTED))) {
+        if (!FAR && (a.slots == 1 || (!a.m && left < LEAST))) {
             typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
             if (a.rb) {
-                const float left = fast_exp2(-total);
                 const uint16_t* e = a.rb + ((bkv % a.Hkv) * (long)a.G + g0 + g) * D + 4 * c;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) s[k] += left * __builtin_bit_cast(float, (uint32_t)e[k] << 16);
             }
             *reinterpret_cast<bf16x4*>(a.o + h * D + 4 * c) = bf16x4{(__bf16)s[0], (__bf16)s[1], (__bf16)s[2], (__bf16)s[3]};
-            if (a.m && c == 0) a.m[h] = -total * SB_LN2;
+            if (a.m && c == 0) a.m[h] = -log * SB_LN2;
         }
         if (a.part_o) {
             *reinterpret_cast<f32x4*>(a.part_o + (h * a.slots + slot) * D + 4 * c) = s;
-            if (c == 0) a.part_a[h * a.slots + slot] = total;
+            if (c == 0) {
+                a.part_a[h * a.slots + slot] = left;
+                if (a.m) a.part_l[h * a.slots + slot] = log;
+            }
         }
     }
 }
@@ -437,9 +475,9 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
         const long bh = blockIdx.x;
         const int n = slots_of(a, up32(length_of(a, (int)(bh / H))));
         const float* pa = a.part_a + bh * a.slots;
-        if (!a.m && a.near > 0 && pa[0] >= CARRY_EXHAUSTED) return;    // finished by the near launch
+        if (!a.m && a.near > 0 && pa[0] < LEAST) return;               // finished by the near launch
         if (a.slots == 1) return;                                      // (so is every head)
-        // slot i is shifted by everything the nearer (lower) slots took
+        // slot i gets what the nearer (lower) slots left
         const int c4 = tid % NV, grp = tid / NV;
         const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + bh * a.slots * D) + c4;
         // all of a thread's share is in flight at once
@@ -449,12 +487,12 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
         for (int i = 0; i < N; ++i) x[i] = grp + i * NG < n ? po[(grp + i * NG) * NV] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         float p[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) p[e] = 2 * lane + e < n ? pa[2 * lane + e] : 0.0f;
-        float total;
-        const float before = wave_prefix(p[0] + p[1], total);
+        for (int e = 0; e < 2; ++e) p[e] = 2 * lane + e < n ? pa[2 * lane + e] : 1.0f;
+        float left;
+        const float before = wave_prefix(p[0] * p[1], left);
         if (wave == 0) {
-            f[2 * lane] = 2 * lane < n ? fast_exp2(-before) : 0.0f;
-            f[2 * lane + 1] = 2 * lane + 1 < n ? fast_exp2(-(before + p[0])) : 0.0f;
+            f[2 * lane] = before;
+            f[2 * lane + 1] = before * p[0];
         }
         __syncthreads();
         f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -466,10 +504,16 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
             float r = 0.0f;
 #pragma unroll
             for (int g = 0; g < NG; ++g) r += ored[g][tid];
-            if (a.rb) r += fast_exp2(-total) * __builtin_bit_cast(float, (uint32_t)a.rb[(bh % H) * D + tid] << 16);
+            if (a.rb) r += left * __builtin_bit_cast(float, (uint32_t)a.rb[(bh % H) * D + tid] << 16);
             const __bf16 val = (__bf16)r;
             a.o[bh * D + tid] = __builtin_bit_cast(uint16_t, val);
-            if (a.m && tid == 0) a.m[bh] = -total * SB_LN2;
+        }
+        if (a.m && wave == 1) {
+            float log = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) log += 2 * lane + e < n ? a.part_l[bh * a.slots + 2 * lane + e] : 0.0f;
+            log = wave_sum(log);
+            if (lane == 0) a.m[bh] = -log * SB_LN2;
         }
         return;
     }
@@ -484,16 +528,16 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
     bool any = false;
     for (int g = wave; g < a.G; g += COMBINE_THREADS / 64) {
         const float* pa = a.part_a + (hq0 + g) * a.slots;
-        float x = 0.0f;
-        for (int i = lane; i < slot; i += 64) x += pa[i];
-        x = wave_sum(x);
+        float x = 1.0f;
+        for (int i = lane; i < slot; i += 64) x *= pa[i];
+        wave_prefix(x, x);
         // the far launch left out the blocks of heads that are all exhausted
         bool there = true;
         if (!a.m && a.near > 0 && slot > 0) {
             const int g0 = g / GMAX * GMAX;
-            there = __builtin_amdgcn_ballot_w64(!(a.part_a[(hq0 + min(g0 + (lane & 15), min(a.G, g0 + GMAX) - 1)) * a.slots] >= CARRY_EXHAUSTED)) != 0;
+            there = __builtin_amdgcn_ballot_w64(!(a.part_a[(hq0 + min(g0 + (lane & 15), min(a.G, g0 + GMAX) - 1)) * a.slots] < LEAST)) != 0;
         }
-        x = there ? fast_exp2(-x) : 0.0f;
+        x = there ? x : 0.0f;
         any |= x != 0.0f;
         if (lane == 0) f[g] = x;
     }
@@ -538,15 +582,23 @@ hipError_t launch_d(Args a, int B, int H, float* workspace, hipStream_t stream)
     if (combine) {
         a.part_o = workspace;
         a.part_a = a.part_o + heads * a.slots * D;
-        if (a.score_out) a.wl = a.part_a + ((heads * a.slots + 3) & ~3L);
+        a.part_l = a.part_a + heads * a.slots;
+        if (a.score_out) a.wl = a.part_a + ((2 * heads * a.slots + 3) & ~3L);
     }
     hipError_t e = hipSuccess;
+    while (1 << a.lg < std::min(a.G, GMAX)) ++a.lg;
     if (a.near > 0) {
-        hipLaunchKernelGGL((decode_kv4_kernel<D, false>), dim3(bkv, 1u, nz), dim3(64 * NEAR_NW), 0, stream, a);
+        const dim3 grid(bkv, 1u, nz), threads(64 * NEAR_NW);
+        if (a.lg == 4) hipLaunchKernelGGL((decode_kv4_kernel<D, false, 1, false>), grid, threads, 0, stream, a);
+        else hipLaunchKernelGGL((decode_kv4_kernel<D, false, 1, true>), grid, threads, 0, stream, a);
         if ((e = hipGetLastError()) != hipSuccess || !combine) return e;
     }
     if (a.slots > (a.near > 0)) {
-        hipLaunchKernelGGL((decode_kv4_kernel<D, true>), dim3((unsigned)(a.slots - (a.near > 0)), bkv, nz), dim3(64 * FAR_NW), 0, stream, a);
+        const dim3 grid((unsigned)(a.slots - (a.near > 0)), bkv, nz), threads(64 * FAR_NW);
+        if (a.lg == 4) hipLaunchKernelGGL((decode_kv4_kernel<D, true, 1, false>), grid, threads, 0, stream, a);
+        else if (a.lg == 3) hipLaunchKernelGGL((decode_kv4_kernel<D, true, 1, true>), grid, threads, 0, stream, a);
+        else if (a.lg == 2) hipLaunchKernelGGL((decode_kv4_kernel<D, true, 2, true>), grid, threads, 0, stream, a);
+        else hipLaunchKernelGGL((decode_kv4_kernel<D, true, 4, true>), grid, threads, 0, stream, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     const unsigned more = a.score_out ? bkv * (unsigned)a.slots : 0u;
@@ -563,7 +615,7 @@ size_t decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d,
 {
     const long heads = (long)B * H;
     const long slots = std::max(split_for(B, H, Hkv, T, false).slots, split_for(B, H, Hkv, T, true).slots);
-    size_t n = (size_t)heads * slots * d + (size_t)((heads * slots + 3) & ~3L);
+    size_t n = (size_t)heads * slots * d + (size_t)((2 * heads * slots + 3) & ~3L);
     if (scores) n += (size_t)heads * Tcap;
     return sizeof(float) * n;
 }
@@ -573,7 +625,7 @@ hipError_t launch_decode_kv4(const uint16_t* q, const uint8_t* kc, const uint8_t
                              int B, int H, int Hkv, int T, int Tcap, int d, hipStream_t stream)
 {
     const Split s = split_for(B, H, Hkv, T, m != nullptr);
-    const Args a = {q, kc, ks, vc, vs, rb, lens, score, score_out, o, m, nullptr, nullptr, nullptr, T, Tcap, Hkv, H / Hkv, s.near, s.C, s.slots};
+    const Args a = {q, kc, ks, vc, vs, rb, lens, score, score_out, o, m, nullptr, nullptr, nullptr, nullptr, T, Tcap, Hkv, H / Hkv, s.near, s.C, s.slots, 0};
     if (d == 32) return launch_d<32>(a, B, H, workspace, stream);
     if (d == 64) return launch_d<64>(a, B, H, workspace, stream);
     return launch_d<128>(a, B, H, workspace, stream);
