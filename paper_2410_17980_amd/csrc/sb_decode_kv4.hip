@@ -11,7 +11,7 @@
 //                    shifts the weights of its keys, sums them over the group's heads and adds the score
 //
 // A workgroup takes its keys from the nearest down in rounds of R tiles of 32 per wave, wave 0 the nearest.
-//   logits   z[key][head] = K q: 16x16x32 bf16 MFMA, A = 16 rows of K, B = the query heads of the group.  A lane loads the D / 8
+//   logits   z[key][head] = K q: 16x16x32 bf16 MFMA, A = 16 rows of K, B = the query heads of the group.  A lane reads the D / 8
 //            bytes of its row that make up one A operand after the other (the order of the columns is free as long as q comes in
 //            the same one), and converts them in registers, the scale with them.  Rows go to the MFMAs so that a lane gets eight
 //            consecutive keys of a head.
@@ -20,8 +20,12 @@
 //            logarithm: the keys' scores are results in fp32.  From less than 2^-126 of it on, weights are subnormal at most and count as zero.
 //   output   O^T[c][head] += V^T w: a lane's eight weights are the B operand as they lie; it loads D / 16 columns of those same
 //            eight rows of V, converts, and an in-register transposition (one v_perm per packed pair) makes the A operands.
-// The 16 columns of the MFMAs are more than most groups have heads.  Their copies of a head take a tile each (R of them), which
-// divides the vector instructions of the weights by R, and the upper 8 bits of a weight or the 8 below (o gets 16 bits of a weight; o itself has
+// Codes and scales come through LDS as whole rows, every wave its own, one round ahead: K's place is asked for again as soon as a round
+// has its logits, V's behind its output.  (Straight to registers it is 14 loads a tile, and 26 registers a tile to hold them: all heads far, B8 H16 T16384, d = 128, 64, 32:
+// 69, 52, 37 us, through LDS with the same rounds 65, 44, 36.)  A near launch of more workgroups than the chip holds takes half as many waves a workgroup, two tiles each:
+// B32 H16 T2000 d128 9.8 -> 8.5 us with no head far, 30.5 -> 24.6 with a third; smaller ones lose by it (B16 H8 T2000 d128 15.2 -> 17.8).
+// The 16 columns of the MFMAs are more than most groups have heads.  Their copies of a head take a tile each (two with up to four heads, R), which
+// halves the vector instructions of the weights (four tiles gain nothing more), and the upper 8 bits of a weight or the 8 below (o gets 16 bits of a weight; o itself has
 // 8), which halves the MFMAs of the output; the columns of a head are added up at the end.
 #include "sb_kernels.h"
 #include "sb_kv4.h"
@@ -35,9 +39,8 @@ constexpr int KW = 32;                 // keys of a tile
 constexpr int NEAR_NW = 8, FAR_NW = 4;
 constexpr int NEAR = KW * NEAR_NW;     // keys of a near launch that has a far one behind it
 constexpr float LEAST = 0x1p-126f;     // of the stick
-constexpr int ALONE = 2048;            // a cache is the near launch's alone up to here
 constexpr int MAXSLOT = 128;           // chunks, the nearest keys among them: two per lane of a wave
-constexpr long FAR_WGS = 4096;         // workgroups of the far launch, all heads together
+constexpr long FAR_WGS = 2048;         // workgroups of the far launch, all heads together
 constexpr int MOST_GROUP = 1024;       // query heads of a kv head where scores are wanted
 constexpr int COMBINE_THREADS = 256;
 
@@ -66,17 +69,18 @@ template <int CTRL> __device__ __forceinline__ float dpp(float x)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
 }
-// sum over the 16 lanes of a row, in all of them
-__device__ __forceinline__ float row_sum(float x)
+// x += what CTRL's lanes have
+template <int CTRL> __device__ __forceinline__ void add_columns(float (&x)[8])
 {
-    x += dpp<0xB1>(x);                 // quad_perm 1, 0, 3, 2
-    x += dpp<0x4E>(x);                 // quad_perm 2, 3, 0, 1
-    x += dpp<0x141>(x);                // row_half_mirror
-    return x + dpp<0x140>(x);          // row_mirror
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] += dpp<CTRL>(x[i]);
 }
 __device__ __forceinline__ float wave_sum(float x)
 {
-    x = row_sum(x);
+    x += dpp<0xB1>(x);
+    x += dpp<0x4E>(x);
+    x += dpp<0x141>(x);
+    x += dpp<0x140>(x);
     float a, b;
     both_halves(x + __shfl_xor(x, 16), a, b);
     return a + b;
@@ -107,78 +111,58 @@ __device__ __forceinline__ void both_rows(float v, float& even, float& odd)
     odd = __builtin_bit_cast(float, (int)sw[1]);
 }
 
-// what a lane loads of a tile
-template <int D> struct KTile {
-    uint32_t k[2][D / 32];             // rows 8 (l16 / 4) + 4 h + l16 % 4: columns lq D / 4 .. + D / 4 - 1
-    uint32_t s[2];                     // and their scale
-};
-template <int D> struct VTile {
-    uint32_t v[8];                     // rows 8 lq + i: columns D / 16 l16 .. + D / 16 - 1
-    uint32_t s[D / 16];                // scales of the eight rows, bytes as they lie
+// A wave's R tiles in LDS, keys ascending: codes of K, of V, scales of K, of V.  A row's place is p = row ^ x, a 16-byte chunk of its
+// codes lies at chunk ^ y, with x and y made of bits 3 and 4 of the row so that neither the rows of K's operands nor those of V's meet in a bank.
+template <int D, int R> struct Place {
+    static constexpr int ROW = D / 2, SROW = D / KV4_BLOCK, CPR = ROW / 16;
+    static constexpr int CODES = KW * R * ROW, SCALES = KW * R * SROW;
+    static constexpr int V = CODES, KS = 2 * CODES, VS = 2 * CODES + SCALES;
+    static constexpr int BYTES = 2 * (CODES + SCALES);
+    static constexpr int CODE_LOADS = (CODES + 1023) / 1024, LOADS = CODE_LOADS + 1;     // of a wave, for either of K and V
+    static constexpr int ROWS_A_LOAD = 1024 / ROW;
+    // x and y of a row
+    static __device__ __forceinline__ int x_of(int row)
+    {
+        const int a = row >> 3 & 3;
+        return D == 128 ? a : D == 64 ? (a >> 1) << 2 | (a & 1) : (a >> 1) << 2;
+    }
+    static __device__ __forceinline__ int y_of(int row) { return D == 128 ? row >> 3 & 3 : D == 64 ? row >> 3 & 1 : 0; }
 };
 
-template <class V> __device__ __forceinline__ V load_as(const uint8_t* p)
+// bytes of LDS as a T
+template <class T> __device__ __forceinline__ T lds_read(uint32_t at)
 {
-    V x;
-    __builtin_memcpy(&x, p, sizeof(V));
-    return x;
+    return *(__attribute__((address_space(3))) const T*)(uintptr_t)at;
 }
-// N words from p on
-template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p)
+template <int N> __device__ __forceinline__ void lds_words(uint32_t (&w)[N], uint32_t at)
 {
     if constexpr (N == 1) {
-        w[0] = load_as<uint32_t>(p);
+        w[0] = lds_read<uint32_t>(at);
     } else if constexpr (N == 2) {
-        const uint2 x = load_as<uint2>(p);
-        w[0] = x.x;
-        w[1] = x.y;
+        const unsigned long long x = lds_read<unsigned long long>(at);
+        w[0] = (uint32_t)x;
+        w[1] = (uint32_t)(x >> 32);
     } else {
 #pragma unroll
         for (int j = 0; j < N; j += 4) {
-            const u32x4 x = load_as<u32x4>(p + 4 * j);
+            const u32x4 x = lds_load16(at + 4 * j);
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[j + i] = x[i];
         }
     }
 }
 
-template <int D> __device__ __forceinline__ void fetch_k(KTile<D>& t, const uint8_t* kc, const uint8_t* ks, int base, int l16, int lq)
+template <bool NT> __device__ __forceinline__ void dma16(uint64_t base, int off, uint32_t lds)
 {
-    constexpr int ROW = D / 2, SROW = D / KV4_BLOCK;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int row = base + 8 * (l16 >> 2) + 4 * h + (l16 & 3);
-        load_words(t.k[h], kc + (long)row * ROW + lq * (ROW / 4));
-        t.s[h] = ks[(long)row * SROW + lq * SROW / 4];
-    }
-}
-template <int D> __device__ __forceinline__ void fetch_v(VTile<D>& t, const uint8_t* vc, const uint8_t* vs, int base, int l16, int lq)
-{
-    constexpr int ROW = D / 2, SROW = D / KV4_BLOCK;
-    const long row = base + 8 * lq;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint8_t* p = vc + (row + i) * ROW + l16 * (ROW / 16);
-        t.v[i] = D == 128 ? load_as<uint32_t>(p) : D == 64 ? load_as<uint16_t>(p) : *p;
-    }
-    load_words(t.s, vs + row * SROW);
-}
-
-// scale of row i, of this lane's columns (exponent bits; what stands below them does not count)
-template <int D> __device__ __forceinline__ uint32_t v_scale(const VTile<D>& t, int i, int l16)
-{
-    constexpr int PER = 128 / D;       // rows in a word
-    // byte of the row's first block: i % PER * D / 32; of this lane's block: + l16 D / 16 / 32
-    const int sh = 24 - 8 * ((i % PER) * (D / KV4_BLOCK)) - 8 * (l16 * (D / 16) / KV4_BLOCK);
-    return (t.s[i / PER] << sh) >> 1;
+    if constexpr (NT) dma16_to_lds_at_nt(base, off, lds);
+    else dma16_to_lds_at(base, off, lds);
 }
 
 // R: tiles of a wave and round.  PIECES: the columns' copies take a weight's upper and lower bits; without, two MFMAs do
-template <int D, bool FAR, int R, bool PIECES>
-__global__ void __launch_bounds__(64 * (FAR ? FAR_NW : NEAR_NW), 2)
+template <int D, bool FAR, int NW, int R, bool PIECES>
+__global__ void __launch_bounds__(64 * NW, 2)
 decode_kv4_kernel(const Args a)
 {
-    constexpr int NW = FAR ? FAR_NW : NEAR_NW;
     constexpr int NTHR = 64 * NW;
     constexpr int NT = NW * R;             // tiles of a round
     constexpr int KEYS = KW * NT;
@@ -186,7 +170,10 @@ decode_kv4_kernel(const Args a)
     constexpr int CH = D / 4;              // 16-byte chunks of a head's columns
     __shared__ __attribute__((aligned(16))) float tot[2][GMAX][NT];      // per round parity: what a tile leaves of the stick
     __shared__ float s_log[NW][GMAX];
-    __shared__ __attribute__((aligned(16))) f32x4 ored[NW * GMAX * CH];
+    using P = Place<D, R>;
+    constexpr int SHARES = NW * GMAX * CH * 16;
+    __shared__ __attribute__((aligned(1024))) char smem[NW * P::BYTES > SHARES ? NW * P::BYTES : SHARES];
+    f32x4* const ored = reinterpret_cast<f32x4*>(smem);                  // once the keys are done
 
     const int bkv = FAR ? blockIdx.y : blockIdx.x;     // entry * Hkv + kv head
     const int g0 = blockIdx.z * GMAX;
@@ -213,11 +200,6 @@ decode_kv4_kernel(const Args a)
         if (!a.m && a.near > 0 && __builtin_amdgcn_ballot_w64(!(a.part_a[head * a.slots] < LEAST)) == 0) return;
     }
 
-    const uint8_t* const kc = a.kc + (long)bkv * a.Tcap * (D / 2);
-    const uint8_t* const vc = a.vc + (long)bkv * a.Tcap * (D / 2);
-    const uint8_t* const ks = a.ks + (long)bkv * a.Tcap * (D / KV4_BLOCK);
-    const uint8_t* const vs = a.vs + (long)bkv * a.Tcap * (D / KV4_BLOCK);
-
     bf16x8 qw[D / 32];                     // B operand
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) qw[s] = *reinterpret_cast<const bf16x8*>(a.q + head * D + lq * (D / 4) + 8 * s);
@@ -227,41 +209,73 @@ decode_kv4_kernel(const Args a)
     for (int e = 0; e < CW; ++e) acc[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     float stick = 1.0f, logs = 0.0f;       // left by the keys already passed; -log2 of what this lane's own keys left
     int par = 0, hi = top;
-    KTile<D> kt[R];
-    VTile<D> vt[R];
-    // tile j of this wave; where that is below lo there is none, and the last one is loaded
-    auto base_of = [&](int j) __attribute__((always_inline)) { return hi - KW * (wave * R + j + 1); };
-    auto valid_of = [&](int j) __attribute__((always_inline)) { return base_of(j) < lo ? 0 : len - base_of(j); };
+
+    // ---- rows to LDS, whole rows of the wave's R tiles at a time; where a tile is below lo there is none, and the last one is loaded
+    const uint64_t kc = scalar_base(a.kc + (long)bkv * a.Tcap * P::ROW), vc = scalar_base(a.vc + (long)bkv * a.Tcap * P::ROW);
+    const uint64_t ks = scalar_base(a.ks + (long)bkv * a.Tcap * P::SROW), vs = scalar_base(a.vs + (long)bkv * a.Tcap * P::SROW);
+    const uint32_t mem = lds_offset(smem) + wave * P::BYTES;
+    auto fetch = [&](uint64_t codes, uint64_t scales, uint32_t at, uint32_t scales_at, int first_row) __attribute__((always_inline)) {
+        const uint64_t cb = codes + (int64_t)first_row * P::ROW, sb = scales + (int64_t)first_row * P::SROW;
+        const int least = lo - first_row;
+#pragma unroll
+        for (int i = 0; i < P::CODE_LOADS; ++i) {
+            const int p = i * P::ROWS_A_LOAD + lane / P::CPR, row = p ^ P::x_of(p);
+            const int off = max(row, least) * P::ROW + (((lane % P::CPR) ^ P::y_of(p)) << 4);
+            if (P::CODES >= 1024 || lane < P::CODES / 16) dma16<FAR>(cb, off, at + i * 1024);
+        }
+        if (lane < P::SCALES / 16) dma16<FAR>(sb, max(lane * (16 / P::SROW), least) * P::SROW, scales_at);
+    };
+    auto first_row_of = [&](int top) __attribute__((always_inline)) { return top - KW * R * (wave + 1); };
+    auto fetch_k = [&](int top) __attribute__((always_inline)) { fetch(kc, ks, mem, mem + P::KS, first_row_of(top)); };
+    auto fetch_v = [&](int top) __attribute__((always_inline)) { fetch(vc, vs, mem + P::V, mem + P::VS, first_row_of(top)); };
+    // where this lane's words are, in a wave's lowest tile (keys ascending: tile j of this wave is R - 1 - j tiles on)
+    auto place = [&](int row, int byte) __attribute__((always_inline)) {
+        return (row ^ P::x_of(row)) * P::ROW + (((byte >> 4) ^ P::y_of(row)) << 4 | (byte & 15));
+    };
+    uint32_t kat[2], vat[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) kat[h] = mem + place(8 * (l16 >> 2) + 4 * h + (l16 & 3), lq * (D / 8));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vat[i] = mem + P::V + place(8 * lq + i, l16 * (D / 32));
+    const uint32_t ksat = mem + P::KS + (8 * (l16 >> 2) + (l16 & 3)) * P::SROW + lq * P::SROW / 4, vsat = mem + P::VS + 8 * lq * P::SROW;
+    const uint32_t vrot = 9 + 8 * (l16 * (D / 16) / KV4_BLOCK);          // rotation that takes a scale byte to bits 30 .. 23
+    // rows of tile j of this wave
+    auto valid_of = [&](int j) __attribute__((always_inline)) {
+        const int base = hi - KW * (wave * R + j + 1);
+        return base < lo ? 0 : len - base;
+    };
 
     // one round; whether another follows
     auto round = [&]() __attribute__((always_inline)) {
         const bool more = hi - KEYS > lo;
         // ---- logits of the lane's eight keys, in base 2
+        dma_wait<P::LOADS>();              // K has landed, V was asked for behind it
         float x[8];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int valid = valid_of(j);
+            const int valid = valid_of(j), on = R - 1 - j;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
-                const uint32_t s = kt[j].s[h] << 23;
+                uint32_t k[D / 32];
+                lds_words(k, kat[h] + on * KW * P::ROW);
+                const uint32_t s = (uint32_t)lds_read<uint8_t>(ksat + (on * KW + 4 * h) * P::SROW) << 23;
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
-                    const uint32_t w = kt[j].k[h][i];
-                    const u32x4 p = {kv4_pair<0>(w, s), kv4_pair<1>(w, s), kv4_pair<2>(w, s), kv4_pair<3>(w, s)};
+                    const u32x4 p = {kv4_pair<0>(k[i], s), kv4_pair<1>(k[i], s), kv4_pair<2>(k[i], s), kv4_pair<3>(k[i], s)};
                     z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p), qw[i], z, 0, 0, 0);
                 }
-                if (valid < KW)
+                if (__builtin_expect(valid < KW, 0)) {
+                    asm volatile("");      // (a branch, not two instructions a logit)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) z[r] = 8 * lq + 4 * h + r < valid ? z[r] : -INFINITY;
+                }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[4 * h + r] = j == 0 || mytile == j ? z[r] : x[4 * h + r];
             }
         }
-        if (more) {
-#pragma unroll
-            for (int j = 0; j < R; ++j) fetch_k<D>(kt[j], kc, ks, max(base_of(j) - KEYS, lo), l16, lq);
-        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the rows have been read)
+        if (more) fetch_k(hi - KEYS);
         // ---- the lane's chain: w[i] = e_i prod_{i' < i} (1 + e_i'), e = sigma / (1 - sigma); norm makes it the weight where the stick is whole
         // before the lane's nearest key, `leave` is what the eight keys leave
         float w[8], norm, leave;
@@ -307,58 +321,45 @@ decode_kv4_kernel(const Args a)
         norm *= before;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] *= norm;
-        if (a.score_out) {
-            const int base = hi - KW * (mine + 1);
-            if (a.wl) {
-                if (first && base >= lo) {
-                    float* p = a.wl + (hq0 + hc) * a.Tcap + base + 8 * lq;
-                    *reinterpret_cast<f32x4*>(p) = f32x4{w[0], w[1], w[2], w[3]};
-                    *reinterpret_cast<f32x4*>(p + 4) = f32x4{w[4], w[5], w[6], w[7]};
-                }
-            } else if constexpr (!FAR) {   // (R = 1)
-                f32x4 s[2];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = row_sum(first ? w[i] : 0.0f);
-                if (l16 < 2 && base >= lo) {
-                    const int key = base + 8 * lq + 4 * l16;
-                    const long at = (long)bkv * a.Tcap + key;
-                    const f32x4 own = l16 ? s[1] : s[0];
-                    if (key + 4 <= len) {
-                        const f32x4 was = a.score ? *reinterpret_cast<const f32x4*>(a.score + at) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                        *reinterpret_cast<f32x4*>(a.score_out + at) = was + own;
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (key + r < len) a.score_out[at + r] = (a.score ? a.score[at + r] : 0.0f) + own[r];
-                    }
-                }
-            }
-        }
         // ---- output
-        bf16x8 w0, w1;
+        // the upper half of a weight's bits is a bf16, what it leaves another one, rounded (16 bits in all; with PIECES each in its own columns)
+        u32x4 w0, w1;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            w0[i] = (__bf16)w[i];
-            const float rest = w[i] - (float)w0[i];
-            if (PIECES) w0[i] = (__bf16)(lower ? rest : w[i]);
-            else w1[i] = (__bf16)rest;
+        for (int i = 0; i < 4; ++i) {
+            const float a0 = w[2 * i], a1 = w[2 * i + 1];
+            const uint32_t u0 = __builtin_bit_cast(uint32_t, a0), u1 = __builtin_bit_cast(uint32_t, a1);
+            w0[i] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
+            const bf16x2 rest = {(__bf16)(a0 - __builtin_bit_cast(float, u0 & 0xffff0000u)), (__bf16)(a1 - __builtin_bit_cast(float, u1 & 0xffff0000u))};
+            w1[i] = __builtin_bit_cast(uint32_t, rest);
+            if (PIECES) w0[i] = lower ? w1[i] : w0[i];
         }
+        if (more) dma_wait<P::LOADS>();    // V has landed
+        else dma_wait<0>();
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int valid = valid_of(j);
-            bf16x8 wb = w0;
+            const int valid = valid_of(j), on = R - 1 - j;
+            u32x4 wb = w0;
             if (R > 1) {
-                u32x4 y = __builtin_bit_cast(u32x4, w0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = mytile == j ? y[i] : 0u;
-                wb = __builtin_bit_cast(bf16x8, y);
+                for (int i = 0; i < 4; ++i) wb[i] = mytile == j ? wb[i] : 0u;
+            }
+            // scales of the eight rows, bytes as they lie: of row i, the byte of this lane's columns to the exponent's place (what stands beside it does not count)
+            constexpr int PER = 128 / D;   // rows in a word
+            uint32_t sw[D / 16];
+            lds_words(sw, vsat + on * KW * P::SROW);
+            if (__builtin_expect(valid < KW, 0)) {
+                asm volatile("");
+                // whatever lies in rows that are not there: a zero weight makes it zero once it is finite
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (8 * lq + i >= valid) sw[i / PER] = PER == 1 ? 0x7f7f7f7fu : (sw[i / PER] & ~(((1u << (32 / PER)) - 1) << (i % PER * (32 / PER)))) | (0x7f7f7f7fu & (((1u << (32 / PER)) - 1) << (i % PER * (32 / PER))));
             }
             uint32_t pv[8][CW / 2];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                uint32_t s = v_scale<D>(vt[j], i, l16);
-                if (valid < KW && 8 * lq + i >= valid) s = 0x3f800000u;        // (whatever lies there, a zero weight makes it zero)
-                const uint32_t v = vt[j].v[i];
+                const uint32_t s = __builtin_amdgcn_alignbit(sw[i / PER], sw[i / PER], vrot + 8 * (i % PER) * P::SROW);
+                const uint32_t at = vat[i] + on * KW * P::ROW;
+                const uint32_t v = D == 128 ? lds_read<uint32_t>(at) : D == 64 ? lds_read<uint16_t>(at) : lds_read<uint8_t>(at);
                 pv[i][0] = kv4_pair<0>(v, s);
                 if constexpr (CW >= 4) pv[i][1] = kv4_pair<1>(v, s);
                 if constexpr (CW >= 8) {
@@ -373,26 +374,57 @@ decode_kv4_kernel(const Args a)
                 for (int i = 0; i < 4; ++i)
                     y[i] = __builtin_amdgcn_perm(pv[2 * i + 1][e >> 1], pv[2 * i][e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
                 const bf16x8 av = __builtin_bit_cast(bf16x8, y);
-                if (!PIECES) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, w1, acc[e], 0, 0, 0);
-                acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, wb, acc[e], 0, 0, 0);
+                if (!PIECES) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, w1), acc[e], 0, 0, 0);
+                acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, wb), acc[e], 0, 0, 0);
             }
         }
-        if (more) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) fetch_v(hi - KEYS);
+        if (a.score_out) {
+            if (a.wl) {
+                const int base = hi - KW * (mine + 1);
+                if (first && base >= lo) {
+                    float* p = a.wl + (hq0 + hc) * a.Tcap + base + 8 * lq;
+                    *reinterpret_cast<f32x4*>(p) = f32x4{w[0], w[1], w[2], w[3]};
+                    *reinterpret_cast<f32x4*>(p + 4) = f32x4{w[4], w[5], w[6], w[7]};
+                }
+            } else if constexpr (!FAR) {
+                // over the heads, 2^lg neighbouring columns; each tile's sums are then in the first column of its copy
 #pragma unroll
-            for (int j = 0; j < R; ++j) fetch_v<D>(vt[j], vc, vs, max(base_of(j) - KEYS, lo), l16, lq);
+                for (int i = 0; i < 8; ++i) w[i] = hc < live ? w[i] : 0.0f;
+                if (a.lg > 0) add_columns<0xB1>(w);        // quad_perm 1, 0, 3, 2
+                if (a.lg > 1) add_columns<0x4E>(w);        // quad_perm 2, 3, 0, 1
+                if (a.lg > 2) add_columns<0x141>(w);       // row_half_mirror
+                if (a.lg > 3) add_columns<0x140>(w);       // row_mirror
+                const int base = hi - KW * (mine + 1), key = base + 8 * lq;
+                if (first && hc == 0 && base >= lo) {
+                    const long at = (long)bkv * a.Tcap + key;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (key + 4 * h + 4 <= len) {
+                            f32x4 x = {w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]};
+                            if (a.score) x += *reinterpret_cast<const f32x4*>(a.score + at + 4 * h);
+                            *reinterpret_cast<f32x4*>(a.score_out + at + 4 * h) = x;
+                        } else {
+#pragma unroll
+                            for (int r = 4 * h; r < 4 * h + 4; ++r)
+                                if (key + r < len) a.score_out[at + r] = (a.score ? a.score[at + r] : 0.0f) + w[r];
+                        }
+                    }
+                }
+            }
         }
         hi -= KEYS;
         par ^= 1;
         return more && (FAR || a.m || __builtin_amdgcn_ballot_w64(!(stick < LEAST)) != 0);
     };
     if (hi > lo) {
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            fetch_k<D>(kt[j], kc, ks, max(base_of(j), lo), l16, lq);
-            fetch_v<D>(vt[j], vc, vs, max(base_of(j), lo), l16, lq);
-        }
+        fetch_k(hi);
+        fetch_v(hi);
         while (round()) {}
     }
+    dma_wait<0>();                         // keys asked for before the end was known
+    barrier_lds();                         // (theirs is the place of the shares)
     // keys that no stick was left for keep their scores
     if (!FAR && a.score_out && !a.wl && a.score_out != a.score)
         for (int i = lo + tid; i < hi; i += NTHR) a.score_out[(long)bkv * a.Tcap + i] = a.score ? a.score[(long)bkv * a.Tcap + i] : 0.0f;
@@ -550,16 +582,45 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
     }
 }
 
+// Workgroups of the near launch that one round of the chip holds: eight waves of 146 registers and 67 KB, 109 and 34 KB, 86 and 18 KB.
+constexpr long round_of(int d) { return d == 128 ? 256 : 512; }
+
+// The cache is the near launch's alone where its rounds (1.4 us each at d = 128, 1.0 below, as long as all its workgroups run at once) take no
+// longer than the two other launches.  Alone / three launches, us, no head far, then a third of the kv heads, then all:
+//   d = 128  B16 H8 T2800 5.8 / 10.1, 19.8 / 16.0, 20.4 / 21.6;  not T4000 5.2 / 10.0, 27.3 / 16.7, 27.7 / 25.8;  B32 H16 T2800 8.5 / 13.9, 32.7 / 31.5, 39.3 / 45.3;
+//            not T4000 8.5 / 13.9, 46 / 37, 55 / 58;  of more than two rounds of workgroups B32 H32 T1300 14.1 / 16.1, 35.5 / 34.5, 43 / 48;  not T2000 14.4 / 16.6, 46 / 39, 58 / 61
+//   d = 64   B32 H16 T2800 6.7 / 13.6, 23.1 / 23.7, 26.4 / 32.1;  not B16 H8 T4000 5.6 / 13.4, 23.0 / 15.3, 23.1 / 19.4, B32 H32 T4000 8.6 / 14.5, 49 / 40, 59 / 64
+//   d = 32   B32 H16 T2800 5.7 / 10.0, 21.3 / 19.5, 22.5 / 25.2;  not T4000 5.6 / 9.9, 29.6 / 21.8, 30.9 / 28.7
+// Where m is wanted every key is read anyway, alone / spread (below): d = 128 B4 H8 T700 7.8 / 7.9, B32 H16 T2000 29.7 / 30.6;  not B4 H8 T1300 12.3 / 8.1, B16 H8 T1300 12.5 / 11.0
+inline int alone_up_to(long wgs, int d, bool want_m)
+{
+    if (want_m) return wgs <= 256 ? 4 * NEAR : 8 * NEAR;
+    return d == 128 && wgs > 2 * round_of(d) ? 6 * NEAR : 13 * NEAR;
+}
+
+// A small cache is spread over the chip, every key read, in two launches: 8 us and 0.16 us per MB beyond 6.  The limits lie where what is lost where no head is
+// far is at most two thirds of what is gained where a third of the kv heads are.  Alone / spread, us, no head far, then a third:
+//   d = 128  B4 H8 T1300 (6 MB) 5.2 / 8.1, 12.2 / 8.1;  T2800 (12 MB) 5.3 / 9.4, 19.3 / 9.3;  not T700 5.4 / 8.1, 7.9 / 8.0;  B16 H8 T1300 (23 MB) 5.2 / 11.0, 12.3 / 11.0
+//   d = 64   B4 H8 T2000 (4 MB) 5.9 / 10.0, 12.7 / 10.0;  not T1300 6.1 / 9.7, 10.5 / 9.7;  B16 H8 T2000 (17 MB) 5.7 / 10.8, 13.2 / 10.9
+//   d = 32   B4 H8 T2800 (3 MB) 5.8 / 9.8, 15.6 / 9.1;  not T1300 5.5 / 9.9, 9.9 / 9.8
+// and beyond what the near launch takes alone, three launches / spread: B16 H8 T4000 d64 (35 MB) 13.4 / 14.3, 15.3 / 14.2;  not d128 (70 MB) 10.0 / 20.9, 16.7 / 20.8
+inline bool spread_small(double cache_bytes, int T, int d)
+{
+    const int rounds = (T + NEAR - 1) / NEAR;
+    return cache_bytes <= std::min(35e6, 1e6 * ((d == 128 ? 3.5 : 2.5) * (rounds - 1) - 11.5));
+}
+
 struct Split {
     int near, C, slots;
 };
-// The nearest keys in the near launch, the rest in chunks of whole rounds.  With m wanted every key is read whatever the nearest
-// ones take: they need no launch of their own.
-Split split_of(long wgs, int T, bool want_m)
+// The nearest keys in the near launch, the rest in chunks of whole rounds.  With m wanted, or spread, the nearest keys need no launch of their own.
+// FAR_WGS 1024 / 2048 / 4096, a third of the kv heads far: B8 H16 T16384 d128 38.5 / 30.0 / 30.6 us, d = 32 30.6 / 23.4 / 21.1, B16 H32 Hkv8 T4096 d128 21.2 / 19.5 / 23.1.
+Split split_of(long wgs, double cache_bytes, int T, int d, bool want_m)
 {
-    if (T <= ALONE) return {(T + 31) & ~31, KW * FAR_NW, 1};
-    Split s = {want_m ? 0 : NEAR, 0, 0};
-    constexpr int unit = KW * FAR_NW;
+    const bool spread = !want_m && spread_small(cache_bytes, T, d);
+    if (T <= alone_up_to(wgs, d, want_m) && !spread) return {(T + 31) & ~31, KW * FAR_NW, 1};
+    Split s = {want_m || spread ? 0 : NEAR, 0, 0};
+    constexpr int unit = 2 * KW * FAR_NW;
     const int far = T + KW - 1 - s.near;
     const long want = std::min((long)MAXSLOT - 1, std::max(1L, FAR_WGS / wgs));
     s.C = (int)(((far + want - 1) / want + unit - 1) / unit * unit);
@@ -567,10 +628,10 @@ Split split_of(long wgs, int T, bool want_m)
     return s;
 }
 
-Split split_for(int B, int H, int Hkv, int T, bool want_m)
+Split split_for(int B, int H, int Hkv, int T, int d, bool want_m)
 {
     const int nz = (H / Hkv + GMAX - 1) / GMAX;
-    return split_of((long)B * Hkv * nz, T, want_m);
+    return split_of((long)B * Hkv * nz, (double)B * Hkv * T * (d + d / 16), T, d, want_m);
 }
 
 template <int D>
@@ -589,16 +650,16 @@ hipError_t launch_d(Args a, int B, int H, float* workspace, hipStream_t stream)
     while (1 << a.lg < std::min(a.G, GMAX)) ++a.lg;
     if (a.near > 0) {
         const dim3 grid(bkv, 1u, nz), threads(64 * NEAR_NW);
-        if (a.lg == 4) hipLaunchKernelGGL((decode_kv4_kernel<D, false, 1, false>), grid, threads, 0, stream, a);
-        else hipLaunchKernelGGL((decode_kv4_kernel<D, false, 1, true>), grid, threads, 0, stream, a);
+        if (a.lg == 4) hipLaunchKernelGGL((decode_kv4_kernel<D, false, NEAR_NW, 1, false>), grid, threads, 0, stream, a);
+        else if (a.lg < 3 && (long)bkv * nz > round_of(D)) hipLaunchKernelGGL((decode_kv4_kernel<D, false, NEAR_NW / 2, 2, true>), grid, dim3(32 * NEAR_NW), 0, stream, a);
+        else hipLaunchKernelGGL((decode_kv4_kernel<D, false, NEAR_NW, 1, true>), grid, threads, 0, stream, a);
         if ((e = hipGetLastError()) != hipSuccess || !combine) return e;
     }
     if (a.slots > (a.near > 0)) {
         const dim3 grid((unsigned)(a.slots - (a.near > 0)), bkv, nz), threads(64 * FAR_NW);
-        if (a.lg == 4) hipLaunchKernelGGL((decode_kv4_kernel<D, true, 1, false>), grid, threads, 0, stream, a);
-        else if (a.lg == 3) hipLaunchKernelGGL((decode_kv4_kernel<D, true, 1, true>), grid, threads, 0, stream, a);
-        else if (a.lg == 2) hipLaunchKernelGGL((decode_kv4_kernel<D, true, 2, true>), grid, threads, 0, stream, a);
-        else hipLaunchKernelGGL((decode_kv4_kernel<D, true, 4, true>), grid, threads, 0, stream, a);
+        if (a.lg == 4) hipLaunchKernelGGL((decode_kv4_kernel<D, true, FAR_NW, 1, false>), grid, threads, 0, stream, a);
+        else if (a.lg == 3) hipLaunchKernelGGL((decode_kv4_kernel<D, true, FAR_NW, 1, true>), grid, threads, 0, stream, a);
+        else hipLaunchKernelGGL((decode_kv4_kernel<D, true, FAR_NW, 2, true>), grid, threads, 0, stream, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     const unsigned more = a.score_out ? bkv * (unsigned)a.slots : 0u;
@@ -614,7 +675,7 @@ int decode_kv4_most_group() { return MOST_GROUP; }
 size_t decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d, bool scores)
 {
     const long heads = (long)B * H;
-    const long slots = std::max(split_for(B, H, Hkv, T, false).slots, split_for(B, H, Hkv, T, true).slots);
+    const long slots = std::max(split_for(B, H, Hkv, T, d, false).slots, split_for(B, H, Hkv, T, d, true).slots);
     size_t n = (size_t)heads * slots * d + (size_t)((2 * heads * slots + 3) & ~3L);
     if (scores) n += (size_t)heads * Tcap;
     return sizeof(float) * n;
@@ -624,7 +685,7 @@ hipError_t launch_decode_kv4(const uint16_t* q, const uint8_t* kc, const uint8_t
                              const int* lens, const float* score, float* score_out, uint16_t* o, float* m, float* workspace,
                              int B, int H, int Hkv, int T, int Tcap, int d, hipStream_t stream)
 {
-    const Split s = split_for(B, H, Hkv, T, m != nullptr);
+    const Split s = split_for(B, H, Hkv, T, d, m != nullptr);
     const Args a = {q, kc, ks, vc, vs, rb, lens, score, score_out, o, m, nullptr, nullptr, nullptr, nullptr, T, Tcap, Hkv, H / Hkv, s.near, s.C, s.slots, 0};
     if (d == 32) return launch_d<32>(a, B, H, workspace, stream);
     if (d == 64) return launch_d<64>(a, B, H, workspace, stream);
