@@ -11,6 +11,8 @@
 //   key_weight_kernel        NW units a workgroup, 64-key tiles through LDS for all of them, from the last unit's diagonal towards key 0
 //   key_weight_small_kernel  one unit a workgroup, its waves 32 keys each, side by side; where there are few units, also split over
 //                            chunks of keys: a first launch finds what each chunk leaves of the sticks, a second one the weights
+#include <cstdlib>
+#include <type_traits>
 #include "sb_kernels.h"
 #include "sb_mma.h"
 
@@ -68,41 +70,54 @@ __device__ __forceinline__ int length_of(const int* lens, int b, int most)
 constexpr float LEAST = 0x1p-126f;     // of the stick
 __device__ __forceinline__ bool none_left(float stick) { return __builtin_amdgcn_ballot_w64(!(stick < LEAST)) == 0; }
 
-// One query's share of a subtile of 32 keys, a half-wave 16 of them: with the stick whole before its nearest key, the weight of
-// key r is w[r] * mine, and `all` is what the 32 leave.  MASK: keys from `visible` on are not seen.
-template <bool MASK>
-__device__ __forceinline__ void weights(const f32x16& s, float c2, int visible, int hh, float (&w)[16], float& mine, float& all)
+// One query's share of N subtiles of 32 keys, the first the nearest, a half-wave 16 keys of each: with the stick whole before a subtile's nearest
+// key, the weight of key r is w[r] * mine, and `all` is what its 32 leave.  MASK: keys from `visible` (of the first; 32 i more of the others) on are
+// not seen.  (N = 2: one subtile's instructions fill the other's waits.)
+template <int N> using f32xn = float __attribute__((ext_vector_type(N)));
+template <bool MASK, int N>
+__device__ __forceinline__ void weights(const f32x16 (&s)[N], float c2, int visible, int hh, float (&w)[N][16], f32xn<N>& mine, f32xn<N>& all)
 {
     // w[r] = W_r e_r, W_{r+1} = W_r + w[r], e = sigma / (1 - sigma): W_r = prod_{r' < r} 1 / (1 - sigma_r')
-    float W = 1.0f;
+    float W[N], most = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        float e = fast_exp2(s[r] * c2);
-        if (MASK) e = r < visible ? e : 0.0f;
-        w[r] = W * e;
-        W += w[r];
-    }
-    float lo, hi;
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(W < 0x1p120f)) == 0, 1)) {
-        both_halves(__builtin_amdgcn_rcpf(W), lo, hi);
-        all = lo * hi;
-        mine = hh ? hi : all;
-        return;
-    }
-    // in the log form
-    float run = 0.0f;
+    for (int i = 0; i < N; ++i) W[i] = 1.0f;
 #pragma unroll
-    for (int r = 15; r >= 0; --r) {
-        const float x = !MASK || r < visible ? s[r] * c2 : -INFINITY;
-        run += sp2(x);
-        w[r] = x - run;
-    }
-    both_halves(run, lo, hi);
-    const float take = hh ? 0.0f : hi;
+    for (int r = 0; r < 16; ++r)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) w[r] = fast_exp2(w[r] - take);
-    mine = 1.0f;
-    all = fast_exp2(-(lo + hi));
+        for (int i = 0; i < N; ++i) {
+            float e = fast_exp2(s[i][r] * c2);
+            if (MASK) e = r < visible + 32 * i ? e : 0.0f;
+            w[i][r] = W[i] * e;
+            W[i] += w[i][r];
+        }
+#pragma unroll
+    for (int i = 0; i < N; ++i) most += W[i];
+    // what the lane's keys leave, and what makes w the weight where the stick is whole before the lane's nearest key
+    float left[N], norm[N];
+    const bool logs = __builtin_amdgcn_ballot_w64(!(most < 0x1p120f)) != 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) left[i] = norm[i] = __builtin_amdgcn_rcpf(W[i]);
+    if (__builtin_expect(logs, 0)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float run = 0.0f;
+#pragma unroll
+            for (int r = 15; r >= 0; --r) {
+                const float x = !MASK || r < visible + 32 * i ? s[i][r] * c2 : -INFINITY;
+                run += sp2(x);
+                w[i][r] = fast_exp2(x - run);
+            }
+            left[i] = fast_exp2(-run);
+            norm[i] = 1.0f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float lo, hi;                          // (the upper half's keys are nearer)
+        both_halves(left[i], lo, hi);
+        all[i] = lo * hi;
+        mine[i] = hh ? norm[i] : norm[i] * hi;
+    }
 }
 
 // the unit's rows and what they see
@@ -162,42 +177,64 @@ template <int D> __device__ __forceinline__ void read_q(bf16x8 (&qf)[D / 16], ui
     }
 }
 
-template <int D> __device__ __forceinline__ f32x16 logits(const bf16x8 (&qf)[D / 16], const uint32_t (&aoff)[D / 16], uint32_t at)
+// of N subtiles at `at` and from there down
+template <int D, int N> __device__ __forceinline__ void logits(f32x16 (&s)[N], const bf16x8 (&qf)[D / 16], const uint32_t (&aoff)[D / 16], uint32_t at)
 {
-    f32x16 s;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[j][r] = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lds_load16(aoff[i] + at)), qf[i], s, 0, 0, 0);
-    return s;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lds_load16(aoff[i] + at - j * Cfg<D>::SUB)), qf[i], s[j], 0, 0, 0);
 }
 
-template <int D>
+// WHAT: 0 the weights of all keys, 1 what a chunk of keys leaves of the sticks, 2 the weights of a chunk
+template <int D, int WHAT>
 __global__ void __launch_bounds__(64 * NW, 2)
 key_weight_kernel(const Args a, int BHkv, int first_wg)
 {
     using C = Cfg<D>;
     constexpr int TILE = 2 * C::SUB, NPW = TILE / 1024 / NW;
-    __shared__ __attribute__((aligned(1024))) char tiles[NW * C::SUB];      // two of K; before that, the units' q
+    __shared__ __attribute__((aligned(1024))) char tiles[2 * TILE];         // of K; before that, the units' q
+    static_assert(2 * TILE == NW * C::SUB, "room for q");
     __shared__ __attribute__((aligned(16))) float csum[2][NW][TK];
     __shared__ __attribute__((aligned(16))) int s_done[2][NW];
 
-    const int wg = first_wg + blockIdx.x;
-    const int bkv = wg % BHkv, grp = a.groups - 1 - wg / BHkv;         // the longest first
+    // The longest first; kv heads turn with every 256 workgroups, so that a CU does not get the same one, which may be the one that reaches far, each time
+    const int wg = first_wg + blockIdx.x, chunk = WHAT ? blockIdx.y : 0;
+    const int grp = a.groups - 1 - wg / BHkv, bkv = (wg % BHkv + wg / 256) % BHkv;
     const int b = bkv / a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, hh = lane >> 5;
     const int len = length_of(a.lens, b, a.T), qlen = length_of(a.qlens, b, a.Tq);
     const int off = len - qlen;                                         // position of query row 0
-    int* const reach = a.reach + ((long)bkv * a.groups + grp) * 2;
-    const Unit u = unit_of(a, grp * NW + wave, bkv, off, qlen, n);
+    const int unit = grp * NW + wave;
+    int* const reach = a.reach + (((long)bkv * a.groups + grp) * a.chunks + chunk) * 2;
+    float* const left = a.left + (((long)bkv * a.groups * NW + unit) * a.chunks) * 32 + n;       // of chunk 0
+    const Unit u = unit_of(a, unit, bkv, off, qlen, n);
     const int last_strip = min((grp * NW + NW - 1) / a.G, (qlen - 1) / 32);            // of the workgroup, with rows in it
-    const int top = grp * NW / a.G * 32 < qlen ? max(0, off + min(32 * last_strip + 32, qlen) - 1) : 0;
-    if (top == 0) {
-        if (tid == 0) reach[0] = reach[1] = 0;
+    const int lo = WHAT ? chunk * a.C : 0;
+    int top = grp * NW / a.G * 32 < qlen ? max(0, off + min(32 * last_strip + 32, qlen) - 1) : 0;
+    if (WHAT) top = min(top, lo + a.C);
+    float stick = u.there ? 1.0f : 0.0f;
+    if (top <= lo) {
+        if (WHAT == 1 && hh == 0) left[chunk * 32] = stick;
+        if (WHAT != 1 && tid == 0) reach[0] = reach[1] = 0;
         return;
+    }
+    if constexpr (WHAT == 2) {
+        for (int c = a.chunks - 1; c > chunk; --c) stick *= left[c * 32];
+        const int done = none_left(stick) ? -1 : 0;
+        if (lane == 0) s_done[0][wave] = done;
+        barrier_lds();
+        if (waves_done(s_done[0])) {
+            if (tid == 0) reach[0] = reach[1] = 0;
+            return;
+        }
     }
 
     const float c2 = SB_LOG2E / sqrtf((float)D);
@@ -229,50 +266,61 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) aoff[s] = smem0 + tile_off_perm<D>(perm_row(n), 2 * s + hh);
 
-    float stick = u.there ? 1.0f : 0.0f;
-    const int jt0 = (top - 1) / TK;
+    const int jt0 = (top - 1) / TK, jend = lo / TK;
     float* const part = a.part + ((long)bkv * a.groups + grp) * a.Tpad;
     auto flush = [&](int jt, int par) __attribute__((always_inline)) {
         if (tid < TK) part[(long)jt * TK + tid] = (csum[par][0][tid] + csum[par][1][tid]) + (csum[par][2][tid] + csum[par][3][tid]);
     };
     stage(jt0, 0);
-    int jt = jt0, par = 0;
-    for (;; --jt, par ^= 1) {
+    int jt = jt0;
+    // tile jt, in buffer PAR; whether another follows
+    auto tile = [&](auto buffer) __attribute__((always_inline)) {
+        constexpr int par = decltype(buffer)::value;
         dma_wait<0>();
         barrier_lds();
         if (jt < jt0) {
-            flush(jt + 1, par ^ 1);
-            if (jt < 0 || waves_done(s_done[par ^ 1])) break;
+            if (WHAT != 1) flush(jt + 1, par ^ 1);
+            if (jt < jend || waves_done(s_done[par ^ 1])) return false;
         }
-        if (jt > 0) stage(jt - 1, par ^ 1);
+        if (jt > jend) stage(jt - 1, par ^ 1);
+        const int base = jt * TK + 32;                     // of the nearer subtile
+        float sum[2] = {0.0f, 0.0f};
+        if (base - 32 < u.some && !none_left(stick)) {
+            f32x16 s[2];
+            logits<D>(s, qf, aoff, par * TILE + C::SUB);
+            float w[2][16];
+            f32xn<2> mine, all;
+            if (base + 32 > u.all) weights<true>(s, c2, u.sees - base - 16 * hh, hh, w, mine, all);
+            else weights<false>(s, c2, 0, hh, w, mine, all);
 #pragma unroll
-        for (int half = 1; half >= 0; --half) {
-            const int base = jt * TK + 32 * half;
-            float sum = 0.0f;
-            if (base < u.some && !none_left(stick)) {
-                const f32x16 s = logits<D>(qf, aoff, par * TILE + half * C::SUB);
-                float w[16], mine, all;
-                if (base + 32 > u.all) weights<true>(s, c2, u.sees - base - 16 * hh, hh, w, mine, all);
-                else weights<false>(s, c2, 0, hh, w, mine, all);
-                mine *= stick;
-                stick *= all;
+            for (int i = 0; i < 2; ++i) {
+                if constexpr (WHAT != 1) {
+                    mine[i] *= stick;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) w[r] *= mine;
-                sum = sums_of_lanes(w, n);
+                    for (int r = 0; r < 16; ++r) w[i][r] *= mine[i];
+                    sum[i] = sums_of_lanes(w[i], n);
+                }
+                stick *= all[i];
             }
-            if ((n & 1) == 0) csum[par][wave][32 * half + 16 * hh + key_of_lane(n)] = sum;
+        }
+        if (WHAT != 1 && (n & 1) == 0) {
+            csum[par][wave][32 + 16 * hh + key_of_lane(n)] = sum[0];
+            csum[par][wave][16 * hh + key_of_lane(n)] = sum[1];
         }
         const int done = none_left(stick) ? -1 : 0;
         if (lane == 0) s_done[par][wave] = done;
-    }
-    if (tid == 0) {
+        --jt;
+        return true;
+    };
+    while (tile(std::integral_constant<int, 0>()) && tile(std::integral_constant<int, 1>())) {}
+    if (WHAT == 1 && hh == 0) left[chunk * 32] = stick;
+    if (WHAT != 1 && tid == 0) {
         reach[0] = (jt + 1) * TK;
         reach[1] = (jt0 + 1) * TK;
     }
 }
 
-// WHAT: 0 the weights of all keys, 1 what a chunk of keys leaves of the sticks, 2 the weights of a chunk
-template <int D, int WHAT>
+template <int D>
 __global__ void __launch_bounds__(64 * SNW, 2)
 key_weight_small_kernel(const Args a)
 {
@@ -280,31 +328,18 @@ key_weight_small_kernel(const Args a)
     __shared__ __attribute__((aligned(1024))) char rows[SNW * C::SUB];      // 32 of K a wave
     __shared__ __attribute__((aligned(1024))) char qrows[C::SUB];
     __shared__ __attribute__((aligned(16))) float prod[2][SNW][32];         // per round parity: what a wave's keys leave
-    const int unit = a.groups - 1 - (int)blockIdx.x, bkv = blockIdx.y, chunk = WHAT ? blockIdx.z : 0;
+    const int unit = a.groups - 1 - (int)blockIdx.x, bkv = blockIdx.y;
     const int b = bkv / a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, hh = lane >> 5;
     const int len = length_of(a.lens, b, a.T), qlen = length_of(a.qlens, b, a.Tq);
     const Unit u = unit_of(a, unit, bkv, len - qlen, qlen, n);
-    const int lo = WHAT ? chunk * a.C : 0;
-    const int top = WHAT ? min(u.some, lo + a.C) : u.some;
-    const long at = ((long)bkv * a.groups + unit) * a.chunks + chunk;
-    int* const reach = a.reach + at * 2;
-    float* const left = a.left + at * 32;
-    const bool first = wave == 0 && hh == 0;
+    int* const reach = a.reach + ((long)bkv * a.groups + unit) * 2;
     float stick = u.there ? 1.0f : 0.0f;
-    if (top <= lo) {
-        if (WHAT == 1 && first) left[n] = stick;
-        if (WHAT != 1 && tid == 0) reach[0] = reach[1] = 0;
+    if (u.some == 0) {
+        if (tid == 0) reach[0] = reach[1] = 0;
         return;
-    }
-    if constexpr (WHAT == 2) {
-        for (int c = a.chunks - 1; c > chunk; --c) stick *= a.left[(at - chunk + c) * 32 + n];
-        if (none_left(stick)) {
-            if (tid == 0) reach[0] = reach[1] = 0;
-            return;
-        }
     }
 
     const float c2 = SB_LOG2E / sqrtf((float)D);
@@ -313,7 +348,7 @@ key_weight_small_kernel(const Args a)
     const uint16_t* const kg = reinterpret_cast<const uint16_t*>(scalar_base(a.k + (long)bkv * a.Tcap * D));
     const char* const mine_at = rows + wave * C::SUB;
     auto fetch = [&](int base) __attribute__((always_inline)) {
-        base = max(base, lo);
+        base = max(base, 0);
         sub_to_lds<D>(kg + (long)base * D, off, len - 1 - base, mine_at, lane);
     };
     // q: every wave some of the loads
@@ -322,7 +357,8 @@ key_weight_small_kernel(const Args a)
         dma16_to_lds_saddr(a.q + (((long)b * a.H + u.head) * a.Tq + r0) * D,
                            min(r, a.Tq - 1 - r0) * C::ROW + (((lane % C::CPR) ^ swz_perm<D>(r)) << 4), qrows + wave * 1024);
     }
-    int hi = (top + 31) & ~31;
+    const int hi0 = (u.some + 31) & ~31;
+    int hi = hi0;
     fetch(hi - 32 * (wave + 1));
     uint32_t aoff[D / 16];
 #pragma unroll
@@ -333,22 +369,23 @@ key_weight_small_kernel(const Args a)
     read_q<D>(qf, lds_offset(qrows), n, hh, u.there);
 
     float* const part = a.part + ((long)bkv * a.groups + unit) * a.Tpad;
-    const int hi0 = hi;
-    for (int par = 0; hi > lo; hi -= 32 * SNW, par ^= 1) {
+    for (int par = 0; hi > 0; par ^= 1) {
         const int base = hi - 32 * (wave + 1);
         dma_wait<0>();
-        const f32x16 s = logits<D>(qf, aoff, 0);
+        f32x16 s[1];
+        logits<D>(s, qf, aoff, 0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the rows have been read)
-        if (hi - 32 * SNW > lo) fetch(base - 32 * SNW);
-        float w[16], mine = 0.0f, all = 1.0f;
-        if (base >= lo) {
+        if (hi > 32 * SNW) fetch(base - 32 * SNW);
+        float w[1][16];
+        f32xn<1> mine = 0.0f, all = 1.0f;
+        if (base >= 0) {
             if (base + 32 > u.all) weights<true>(s, c2, u.sees - base - 16 * hh, hh, w, mine, all);
             else weights<false>(s, c2, 0, hh, w, mine, all);
         } else {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) w[r] = 0.0f;
+            for (int r = 0; r < 16; ++r) w[0][r] = 0.0f;
         }
-        if (hh == 0) prod[par][wave][n] = all;
+        if (hh == 0) prod[par][wave][n] = all[0];
         barrier_lds();
         float before = stick;
 #pragma unroll
@@ -357,23 +394,18 @@ key_weight_small_kernel(const Args a)
             if (j < wave) before *= p;
             stick *= p;
         }
-        if constexpr (WHAT != 1) {
-            if (base >= lo) {
-                mine *= before;
+        if (base >= 0) {
+            mine[0] *= before;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) w[r] *= mine;
-                const float sum = sums_of_lanes(w, n);
-                if ((n & 1) == 0) part[base + 16 * hh + key_of_lane(n)] = sum;
-            }
+            for (int r = 0; r < 16; ++r) w[0][r] *= mine[0];
+            const float sum = sums_of_lanes(w[0], n);
+            if ((n & 1) == 0) part[base + 16 * hh + key_of_lane(n)] = sum;
         }
-        if (none_left(stick)) {
-            hi -= 32 * SNW;
-            break;
-        }
+        hi -= 32 * SNW;
+        if (none_left(stick)) break;
     }
-    if (WHAT == 1 && first) left[n] = stick;
-    if (WHAT != 1 && tid == 0) {
-        reach[0] = max(hi, lo);
+    if (tid == 0) {
+        reach[0] = max(hi, 0);
         reach[1] = hi0;
     }
     dma_wait<0>();                             // (rows asked for before the end was known)
@@ -420,20 +452,23 @@ struct Plan {
     bool small;
     int groups, chunks, C;
     int Tpad;
-    size_t floats(int BHkv) const { return (size_t)BHkv * groups * ((size_t)Tpad + (size_t)chunks * (2 + (chunks > 1 ? 32 : 0))); }
+    int units() const { return small ? groups : groups * NW; }
+    size_t floats(int BHkv) const { return (size_t)BHkv * ((size_t)groups * (Tpad + 2 * (size_t)chunks) + (chunks > 1 ? (size_t)units() * chunks * 32 : 0)); }
 };
 Plan plan_of(int B, int H, int Hkv, int Tq, int T)
 {
     const int G = H / Hkv, units = (Tq + 31) / 32 * G, Tpad = (T + TK - 1) / TK * TK;
     const long all = (long)B * Hkv * units;
-    Plan p = {all <= 1024, 0, 1, Tpad, Tpad};
+    const char* e1 = getenv("KW_SMALL"); const char* e2 = getenv("KW_WGS");
+    Plan p = {all <= 1024 && T <= 1280, 0, 1, Tpad, Tpad};
+    if (e1) p.small = atoi(e1) == 1;
     p.groups = p.small ? units : (units + NW - 1) / NW;
-    if (p.small) {
-        constexpr int round = 32 * SNW;
-        const int rounds = (T + round - 1) / round;
-        const int want = (int)std::max(1L, std::min<long>(rounds / 2, 1024 / all));
+    if (!p.small) {
+        const long wgs = (long)B * Hkv * p.groups;
+        const int tiles = Tpad / TK;
+        const int want = (int)std::max(1L, std::min<long>(tiles / 2, (e2 ? atol(e2) : 768) / wgs));
         if (want > 1) {
-            p.C = (rounds + want - 1) / want * round;
+            p.C = (tiles + want - 1) / want * TK;
             p.chunks = (T + p.C - 1) / p.C;
         }
         if (p.chunks == 1) p.C = Tpad;
@@ -443,19 +478,19 @@ Plan plan_of(int B, int H, int Hkv, int Tq, int T)
 
 template <int D> hipError_t launch_d(const Args& a, const Plan& p, int BHkv, hipStream_t stream)
 {
-    if (!p.small)
-        return launch_workgroups((long)BHkv * a.groups, 64 * NW, [&](unsigned wgs, int first) {
-            hipLaunchKernelGGL((key_weight_kernel<D>), dim3(wgs), dim3(64 * NW), 0, stream, a, BHkv, first);
-        });
-    const dim3 grid((unsigned)a.groups, (unsigned)BHkv, (unsigned)a.chunks), threads(64 * SNW);
-    if (a.chunks == 1) {
-        hipLaunchKernelGGL((key_weight_small_kernel<D, 0>), grid, threads, 0, stream, a);
+    if (p.small) {
+        hipLaunchKernelGGL((key_weight_small_kernel<D>), dim3((unsigned)a.groups, (unsigned)BHkv), dim3(64 * SNW), 0, stream, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((key_weight_small_kernel<D, 1>), grid, threads, 0, stream, a);
+    if (a.chunks == 1)
+        return launch_workgroups((long)BHkv * a.groups, 64 * NW, [&](unsigned wgs, int first) {
+            hipLaunchKernelGGL((key_weight_kernel<D, 0>), dim3(wgs), dim3(64 * NW), 0, stream, a, BHkv, first);
+        });
+    const dim3 grid((unsigned)(BHkv * a.groups), (unsigned)a.chunks), threads(64 * NW);
+    hipLaunchKernelGGL((key_weight_kernel<D, 1>), grid, threads, 0, stream, a, BHkv, 0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((key_weight_small_kernel<D, 2>), grid, threads, 0, stream, a);
+    hipLaunchKernelGGL((key_weight_kernel<D, 2>), grid, threads, 0, stream, a, BHkv, 0);
     return hipGetLastError();
 }
 
@@ -473,7 +508,7 @@ hipError_t launch_key_weight(const uint16_t* q, const uint16_t* k, const int* le
     const int BHkv = B * Hkv;
     Args a = {q, k, lens, qlens, score, score_out, workspace, nullptr, nullptr, H, Hkv, H / Hkv, Tq, T, Tcap, p.Tpad, p.groups, p.chunks, p.C};
     a.left = workspace + (size_t)BHkv * p.groups * p.Tpad;
-    a.reach = reinterpret_cast<int*>(a.left + (p.chunks > 1 ? (size_t)BHkv * p.groups * p.chunks * 32 : 0));
+    a.reach = reinterpret_cast<int*>(a.left + (p.chunks > 1 ? (size_t)BHkv * p.units() * p.chunks * 32 : 0));
     const hipError_t e = d == 32 ? launch_d<32>(a, p, BHkv, stream) : d == 64 ? launch_d<64>(a, p, BHkv, stream) : launch_d<128>(a, p, BHkv, stream);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(key_weight_sum_kernel, dim3((unsigned)((T + 63) / 64), (unsigned)BHkv), dim3(SUM_THREADS), 0, stream, a);
