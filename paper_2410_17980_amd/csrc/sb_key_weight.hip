@@ -11,7 +11,6 @@
 //   key_weight_kernel        NW units a workgroup, 64-key tiles through LDS for all of them, from the last unit's diagonal towards key 0
 //   key_weight_small_kernel  one unit a workgroup, its waves 32 keys each, side by side; where there are few units, also split over
 //                            chunks of keys: a first launch finds what each chunk leaves of the sticks, a second one the weights
-#include <cstdlib>
 #include <type_traits>
 #include "sb_kernels.h"
 #include "sb_mma.h"
@@ -455,22 +454,27 @@ struct Plan {
     int units() const { return small ? groups : groups * NW; }
     size_t floats(int BHkv) const { return (size_t)BHkv * ((size_t)groups * (Tpad + 2 * (size_t)chunks) + (chunks > 1 ? (size_t)units() * chunks * 32 : 0)); }
 };
+// What a plan takes, from measurements (all heads far; us).  One unit a workgroup: 1.25 for a round of 256 keys, of the longest unit alone where the
+// units fit the chip, 256 of them at a time beyond.  Four units: 1.4 for a tile of 64 keys of the longest, or 0.45 ns a subtile of all, whichever is more.  Chunks of
+// keys in two launches: 8 more, 0.8 ns a subtile.  Measured with all heads far, one unit / four units / chunks (768 workgroups):
+//   B4 H12 Hkv4 T2048 d128, whole prompt 73 / 52;  B8 H16 T2048 d64 156 / 95;  B1 H12 Hkv4 T3000 d64 36 / 55 / 59;  B1 H4 T4000 d128 38 / 84 / 50;
+//   B2 H16 Hkv8 T700 d128 16.5 / 19 / 19;  64 rows of B1 H32 Hkv8 T16384 d128 - / 309 / 39;  one row of B1 H32 Hkv8 T4000 d128 27 / 80 / 17
 Plan plan_of(int B, int H, int Hkv, int Tq, int T)
 {
     const int G = H / Hkv, units = (Tq + 31) / 32 * G, Tpad = (T + TK - 1) / TK * TK;
-    const long all = (long)B * Hkv * units;
-    const char* e1 = getenv("KW_SMALL"); const char* e2 = getenv("KW_WGS");
-    Plan p = {all <= 1024 && T <= 1280, 0, 1, Tpad, Tpad};
-    if (e1) p.small = atoi(e1) == 1;
-    p.groups = p.small ? units : (units + NW - 1) / NW;
-    if (!p.small) {
-        const long wgs = (long)B * Hkv * p.groups;
-        const int tiles = Tpad / TK;
-        const int want = (int)std::max(1L, std::min<long>(tiles / 2, (e2 ? atol(e2) : 768) / wgs));
-        if (want > 1) {
-            p.C = (tiles + want - 1) / want * TK;
-            p.chunks = (T + p.C - 1) / p.C;
-        }
+    const double all = (double)B * Hkv * units, mean = (T - 0.5 * Tq) / T;            // share of the keys that a query sees in the mean
+    const double subtiles = all * mean * T / 32.0;
+    const double small = 1.25 * (T / 256 + 1) * std::max(1.0, all * mean / 256.0);
+    Plan p = {false, (units + NW - 1) / NW, 1, Tpad, Tpad};
+    const long wgs = (long)B * Hkv * p.groups;
+    const int tiles = Tpad / TK;
+    const int want = (int)std::max(1L, std::min<long>(tiles / 2, 768 / wgs));
+    if (small <= (want > 1 ? 8.0 + 0.0008 * subtiles : std::max(1.4 * tiles, 0.00045 * subtiles))) {
+        p.small = true;
+        p.groups = units;
+    } else if (want > 1) {
+        p.C = (tiles + want - 1) / want * TK;
+        p.chunks = (T + p.C - 1) / p.C;
         if (p.chunks == 1) p.C = Tpad;
     }
     return p;
