@@ -574,11 +574,18 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
         if (lane == 0) f[g] = x;
     }
     if (!__syncthreads_or(any) && a.score_out == a.score) return;
-    for (int i = lo + tid; i < min(top, len); i += COMBINE_THREADS) {
-        float s = a.score ? a.score[(long)bkv * a.Tcap + i] : 0.0f;
+    const long row = (long)bkv * a.Tcap;
+    for (int i = lo + 4 * tid; i < min(top, len); i += 4 * COMBINE_THREADS) {
+        f32x4 s = a.score ? *reinterpret_cast<const f32x4*>(a.score + row + i) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         for (int g = 0; g < a.G; ++g)
-            if (f[g] != 0.0f) s = __builtin_fmaf(f[g], a.wl[(hq0 + g) * a.Tcap + i], s);
-        a.score_out[(long)bkv * a.Tcap + i] = s;
+            if (f[g] != 0.0f) s += f[g] * *reinterpret_cast<const f32x4*>(a.wl + (hq0 + g) * a.Tcap + i);
+        if (i + 4 <= len) {
+            *reinterpret_cast<f32x4*>(a.score_out + row + i) = s;
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (i + r < len) a.score_out[row + i + r] = s[r];
+        }
     }
 }
 

@@ -3,8 +3,8 @@
 // what is left is a cache as any other).
 //
 //   select   a workgroup per (entry, kv head): the smallest score that stays, by its bits from the highest eleven down (radix
-//            selection: a histogram in LDS each), then the places of the rows that stay by prefix sums.  Up to 16384 scores stay in registers
-//            throughout, longer ones are read again for each step, from L2.
+//            selection: a histogram in LDS each), then the places of the rows that stay by prefix sums.  Up to 65536 scores stay in registers
+//            throughout, more are read again for each step, from L2.
 //   move     the rows of every array to their places: bound by HBM, 2 x the bytes that stay.
 #include "sb_kernels.h"
 
@@ -58,7 +58,7 @@ evict_select_kernel(const float* __restrict__ score, const int* __restrict__ len
     constexpr int BLOCK = PER * SEL_THREADS;
     constexpr int BINS = 2 * SEL_THREADS;
     __shared__ uint32_t hist[BINS];
-    __shared__ uint32_t s_wave[SEL_NW], s_prefix, s_left;
+    __shared__ uint32_t s_wave[SEL_NW], s_prefix, s_left, s_whole;
     __shared__ uint32_t s_count[PER * SEL_NW + 1];                // per 64 scores in turn: those above the threshold, and (<< 16) equal to it
     const int bkv = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int len = lens ? min(max(lens[bkv / Hkv], 0), T) : T;
@@ -90,9 +90,11 @@ evict_select_kernel(const float* __restrict__ score, const int* __restrict__ len
     if (few == 0) return;
 
     uint32_t prefix = 0, left = (uint32_t)few;                    // bits known so far; how many stay of those that share them
+    bool whole = false;                                           // all of those: no more bits are needed
 #pragma unroll
     for (int step = 0; step < 3; ++step) {
         const int shift = step == 0 ? 21 : step == 1 ? 10 : 0;    // 11, 11 and 10 bits
+        if (whole) break;
         hist[tid] = hist[tid + SEL_THREADS] = 0;
         __syncthreads();
         for (int i0 = 0; i0 < older; i0 += BLOCK) {
@@ -126,10 +128,16 @@ evict_select_kernel(const float* __restrict__ score, const int* __restrict__ len
             const bool second = before + h0 < left;
             s_prefix = prefix | (uint32_t)(BINS - 1 - 2 * tid - second) << shift;
             s_left = left - before - (second ? h0 : 0u);
+            s_whole = s_left == (second ? h1 : h0);
         }
         __syncthreads();
         prefix = s_prefix;
         left = s_left;
+        whole = s_whole != 0;
+    }
+    if (whole) {                                                  // everything from there up stays (prefix is above zero: a rank is 2^22 at least)
+        --prefix;
+        left = 0;
     }
 
     // places: those above `prefix`, and the first `left` equal to it
@@ -220,6 +228,7 @@ hipError_t launch_evict(const float* score, const int* lens, const void* const* 
     };
     if (T <= 4 * SEL_THREADS) select(evict_select_kernel<4, true>);
     else if (T <= 16 * SEL_THREADS) select(evict_select_kernel<16, true>);
+    else if (T <= 64 * SEL_THREADS) select(evict_select_kernel<64, true>);
     else select(evict_select_kernel<16, false>);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || arrays == 0) return e;

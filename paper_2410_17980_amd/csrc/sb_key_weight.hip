@@ -202,9 +202,10 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     __shared__ __attribute__((aligned(16))) float csum[2][NW][TK];
     __shared__ __attribute__((aligned(16))) int s_done[2][NW];
 
-    // The longest first; kv heads turn with every 256 workgroups, so that a CU does not get the same one, which may be the one that reaches far, each time
+    // The longest first; kv heads turn as workgroups go round the chip, so that a CU does not get the same one, which may be the one that reaches far, each time
     const int wg = first_wg + blockIdx.x, chunk = WHAT ? blockIdx.y : 0;
-    const int grp = a.groups - 1 - wg / BHkv, bkv = (wg % BHkv + wg / 256) % BHkv;
+    const int turn = wg / BHkv, grp = a.groups - 1 - turn;
+    const int bkv = (wg % BHkv + (int)((long)turn * BHkv / 256 % BHkv)) % BHkv;
     const int b = bkv / a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -102,6 +102,12 @@ def test_grouped_heads(sb, oracle, gen, H, Hkv):
     check(sb, oracle, *activations(gen, 1, H, Hkv, 150, 150, 64, seed=H))
 
 
+@pytest.mark.parametrize("B,H,Hkv,T,d", [(22, 12, 4, 261, 64), (27, 12, 12, 150, 32), (16, 64, 8, 70, 32), (9, 56, 7, 130, 128), (5, 90, 45, 200, 64)])
+def test_grids_of_many_units(sb, oracle, gen, B, H, Hkv, T, d):
+    """Four units a workgroup, more workgroups than the chip holds, kv heads that do and do not divide the chip: every head is there once."""
+    check(sb, oracle, *activations(gen, B, H, Hkv, T, T, d, seed=B))
+
+
 @pytest.mark.parametrize("kind", ["far", "sharp", "near"])
 @pytest.mark.parametrize("d", [32, 128])
 def test_kinds_of_heads(sb, oracle, gen, kind, d):
