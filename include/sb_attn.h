@@ -47,7 +47,7 @@ typedef enum {
     SB_ERR_ALIGN = -4,       /* a pointer is not 16-byte aligned */
     SB_ERR_LAUNCH = -5,      /* the HIP launch reported an error */
     SB_ERR_WORKSPACE = -6,   /* workspace missing or too small */
-    SB_ERR_OVERLAP = -7      /* an output overlaps an input that is still read */
+    SB_ERR_OVERLAP = -7      /* an output overlaps an input or another output */
 } sb_status;
 
 /*
@@ -265,8 +265,10 @@ int sb_attn_kv4_load(const void* kc, const void* ks, const void* vc, const void*
  * empty, o is 0 (r with the bias) and m is 0.  Rows behind an entry's last are not looked at.
  * score_out: optional fp32 [B, Hkv, Tcap].  score_out[b,h,i] = score[b,h,i] + sum over the query
  * heads of kv head h of A[i], for the entry's rows i; others are left as they were.  score may be
- * NULL (zeros) and may be score_out itself.  At most 1024 query heads a kv head with score_out.
- * The weights that meet V are rounded to 16 bits (o itself has 8); score gets them in fp32.
+ * NULL (zeros) and may be score_out itself, but not overlap it otherwise (SB_ERR_OVERLAP).  At most
+ * 1024 query heads a kv head and B*H <= 8388607 with score_out (16777215 without).
+ * The weights that meet V are rounded to 16 bits (o itself has 8); score gets them in fp32.  Rows of
+ * which less than 2^-126 of the stick is left count as zero, a NaN among them too, as long as m is not wanted.
  * workspace: sb_attn_decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, score_out != NULL) bytes.
  * Bit-reproducible, as sb_attn_decode.
  */
@@ -278,14 +280,15 @@ int sb_attn_decode_kv4(const void* q, const void* kc, const void* ks, const void
 /*
  * The weight that a prompt's queries give each key: score_out[b,h,i] = score[b,h,i] + sum over query
  * rows j and the query heads of kv head h of A[i,j] (Eq. 1), for the entry's rows i; others are left
- * as they were.  score may be NULL (zeros) and may be score_out itself.
+ * as they were.  score may be NULL (zeros) and may be score_out itself, but not overlap it otherwise
+ * (SB_ERR_OVERLAP).  Keys of which a query has less than 2^-126 of its stick left get nothing from it.
  * q: bf16 [B, H, Tq, d]; k: bf16 [B, Hkv, Tcap, d].  lens, qlens: B ints each on the DEVICE, the rows
  * and the query rows of every entry, or NULL: T, Tq (clamped to 0 .. T and 0 .. Tq; what lies behind
  * them is not looked at).  The queries are those of the entry's last rows: query row t < qlens[b]
  * stands at row lens[b] - qlens[b] + t and weighs the keys before it.  Tq = T: the whole prompt;
  * Tq = 1, its key appended already: one token.  1 <= Tq <= T <= Tcap, T <= 524288, B*Hkv <= 65535.
- * workspace: sb_attn_key_weight_workspace_bytes(B, H, Hkv, Tq, T, d) bytes: 4*(T+63) for each 128 query
- * rows of each group.  Bit-reproducible.
+ * workspace: sb_attn_key_weight_workspace_bytes(B, H, Hkv, Tq, T, d) bytes, about 4*T for each 128 query
+ * rows of a head (for each 32 where there are few).  Bit-reproducible.
  */
 size_t sb_attn_key_weight_workspace_bytes(int B, int H, int Hkv, int Tq, int T, int d);
 int sb_attn_key_weight(const void* q, const void* k, const int* lens, const int* qlens, const float* score, float* score_out,
@@ -301,7 +304,8 @@ int sb_attn_key_weight(const void* q, const void* k, const int* lens, const int*
  * score to score_out [B, Hkv, Tcap_out]; what lies behind them is left as it was.  src, dst and
  * row_bytes (1 .. 65536) are HOST arrays, read before the call returns.  index [B, Hkv, keep]: the rows that
  * stayed, ascending, then -1.  lens_out [B]: the rows left, min(lens[b], keep).
- * 1 <= keep <= Tcap_out, 0 <= recent <= keep.  No output may overlap an input (SB_ERR_OVERLAP).
+ * 1 <= keep <= Tcap_out, 0 <= recent <= keep.  No output may overlap an input or another output
+ * (SB_ERR_OVERLAP).
  */
 int sb_attn_evict(const float* score, const int* lens, const void* const* src, void* const* dst, const int* row_bytes, int arrays,
                   float* score_out, int* index, int* lens_out, int B, int Hkv, int T, int Tcap, int Tcap_out, int keep, int recent, void* stream);

@@ -303,7 +303,8 @@ def sb_attn_decode_kv4(q, kc, ks, vc, vs, T=None, lens=None, r=None, score=None,
                        workspace=None, stream=None):
     """Single-token decode on a 4-bit cache: q [B,H,d] against the first lens[b] rows of entry b (int32 [B] on the
     GPU, at most T; T, which defaults to Tcap, when not given).  score_out [B,Hkv,Tcap] fp32 (score itself where only that
-    is given) = score + the weight that the token gives each of those rows; score alone may be left out (zeros).
+    is given) = score + the weight that the token gives each of those rows; score alone may be left out (zeros).  Scores of rows
+    behind them are left as they were: a row that is appended starts with what its place holds (usually a 0 that the caller writes).
     Returns o [B,H,d] (bf16), or a tuple of it and, as far as they are wanted, m and score_out."""
     return (_ext or _load_ext()).decode_kv4(q, kc, ks, vc, vs, T, lens, r, score, score_out, o, m, want_m, workspace, stream)
 
@@ -315,7 +316,8 @@ def sb_attn_key_weight_workspace_bytes(B, H, Hkv, Tq, T, d) -> int:
 def sb_attn_key_weight(q, k, T=None, lens=None, qlens=None, score=None, score_out=None, workspace=None, stream=None):
     """The weight that the queries q [B,H,Tq,d] of an entry's last rows give its keys, the first lens[b] rows of
     k [B,Hkv,Tcap,d] (at most T, which defaults to Tcap); qlens[b] of the query rows count.  Returns score_out [B,Hkv,Tcap]
-    fp32 = score (zeros when not given) + that weight; score is updated in place where only that is given."""
+    fp32 = score (zeros when not given) + that weight; score is updated in place where only that is given.  Scores behind an
+    entry's rows are left as they were, undefined where the tensor is new."""
     return (_ext or _load_ext()).key_weight(q, k, T, lens, qlens, score, score_out, workspace, stream)
 
 

@@ -341,11 +341,27 @@ int sb_attn_kv4_load(const void* kc, const void* ks, const void* vc, const void*
 }
 
 namespace {
+bool overlap(const void* a, double a_bytes, const void* b, double b_bytes)
+{
+    const double x = (double)reinterpret_cast<uintptr_t>(a), y = (double)reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
+// scores [B, Hkv, Tcap] are read where they are written, or somewhere else altogether
+bool scores_overlap(const float* score, const float* score_out, int B, int Hkv, int Tcap)
+{
+    const double n = 4.0 * B * Hkv * Tcap;
+    return score && score != score_out && overlap(score, n, score_out, n);
+}
+
 int check_decode_kv4(int B, int H, int Hkv, int T, int Tcap, int d, bool scores)
 {
     if (H < 1 || Hkv < 1 || H % Hkv != 0 || T < 1 || Tcap < T || T > sb::decode_max_T()) return SB_ERR_SHAPE;
     if (int rc = check_kv4(B, Hkv, Tcap, d)) return rc;
-    if ((double)B * H > 16777215.0 || (double)B * H * (double)Tcap * d >= 1099511627776.0 || (scores && H / Hkv > sb::decode_kv4_most_group())) return SB_ERR_SHAPE;
+    // (a launch takes fewer than 2^32 threads along x: 256 a head, and with scores as many for each of up to 128 chunks of a kv head; 65535 blocks of 16 heads along z)
+    if ((double)B * H > (scores ? 8388607.0 : 16777215.0) || (double)B * H * (double)Tcap * d >= 1099511627776.0 || H / Hkv > 16 * 65535 ||
+        (scores && H / Hkv > sb::decode_kv4_most_group()))
+        return SB_ERR_SHAPE;
     return SB_OK;
 }
 }  // namespace
@@ -365,6 +381,7 @@ int sb_attn_decode_kv4(const void* q, const void* kc, const void* ks, const void
     if (!aligned16(q) || !aligned16(kc) || !aligned16(ks) || !aligned16(vc) || !aligned16(vs) || !aligned16(r) || !aligned16(lens) ||
         !aligned16(score) || !aligned16(score_out) || !aligned16(o) || !aligned16(m) || !aligned16(workspace))
         return SB_ERR_ALIGN;
+    if (scores_overlap(score, score_out, B, Hkv, Tcap)) return SB_ERR_OVERLAP;
     if (!workspace || workspace_bytes < sb::decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, score_out != nullptr)) return SB_ERR_WORKSPACE;
     hipError_t e = sb::launch_decode_kv4(static_cast<const uint16_t*>(q), in_bytes(kc), in_bytes(ks), in_bytes(vc), in_bytes(vs), static_cast<const uint16_t*>(r),
                                          lens, score, score_out, static_cast<uint16_t*>(o), m, static_cast<float*>(workspace),
@@ -396,19 +413,12 @@ int sb_attn_key_weight(const void* q, const void* k, const int* lens, const int*
     if (int rc = check_key_weight(B, H, Hkv, Tq, T, Tcap, d)) return rc;
     if (!aligned16(q) || !aligned16(k) || !aligned16(lens) || !aligned16(qlens) || !aligned16(score) || !aligned16(score_out) || !aligned16(workspace))
         return SB_ERR_ALIGN;
+    if (scores_overlap(score, score_out, B, Hkv, Tcap)) return SB_ERR_OVERLAP;
     if (!workspace || workspace_bytes < sb::key_weight_workspace_bytes(B, H, Hkv, Tq, T)) return SB_ERR_WORKSPACE;
     hipError_t e = sb::launch_key_weight(static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), lens, qlens, score, score_out,
                                          static_cast<float*>(workspace), B, H, Hkv, Tq, T, Tcap, d, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SB_OK : SB_ERR_LAUNCH;
 }
-
-namespace {
-bool overlap(const void* a, double a_bytes, const void* b, double b_bytes)
-{
-    const double x = (double)reinterpret_cast<uintptr_t>(a), y = (double)reinterpret_cast<uintptr_t>(b);
-    return x < y + b_bytes && y < x + a_bytes;
-}
-}  // namespace
 
 int sb_attn_evict(const float* score, const int* lens, const void* const* src, void* const* dst, const int* row_bytes, int arrays,
                   float* score_out, int* index, int* lens_out, int B, int Hkv, int T, int Tcap, int Tcap_out, int keep, int recent, void* stream)
@@ -427,13 +437,25 @@ int sb_attn_evict(const float* score, const int* lens, const void* const* src, v
         if (row_bytes[i] < 1 || row_bytes[i] > 65536) return SB_ERR_SHAPE;
         if (!aligned16(src[i]) || !aligned16(dst[i])) return SB_ERR_ALIGN;
     }
-    // rows move while others are still read
-    if (overlap(score, 4.0 * rows, score_out, 4.0 * rows_out) || (lens && overlap(lens, 4.0 * B, lens_out, 4.0 * B))) return SB_ERR_OVERLAP;
-    for (int i = 0; i < arrays; ++i)
-        for (int j = 0; j < arrays; ++j)
-            if (overlap(src[i], rows * row_bytes[i], dst[j], rows_out * row_bytes[j]) ||
-                (i < j && overlap(dst[i], rows_out * row_bytes[i], dst[j], rows_out * row_bytes[j])))
-                return SB_ERR_OVERLAP;
+    // rows move while others are still read: no output in an input or in another output
+    struct Span { const void* p; double bytes; };
+    Span in[sb::EVICT_ARRAYS + 2], out[sb::EVICT_ARRAYS + 3];
+    int ins = 0, outs = 0;
+    in[ins++] = {score, 4.0 * rows};
+    if (lens) in[ins++] = {lens, 4.0 * B};
+    out[outs++] = {score_out, 4.0 * rows_out};
+    out[outs++] = {index, 4.0 * B * Hkv * keep};
+    out[outs++] = {lens_out, 4.0 * B};
+    for (int i = 0; i < arrays; ++i) {
+        in[ins++] = {src[i], rows * row_bytes[i]};
+        out[outs++] = {dst[i], rows_out * row_bytes[i]};
+    }
+    for (int i = 0; i < outs; ++i) {
+        for (int j = 0; j < ins; ++j)
+            if (overlap(out[i].p, out[i].bytes, in[j].p, in[j].bytes)) return SB_ERR_OVERLAP;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return SB_ERR_OVERLAP;
+    }
     hipError_t e = sb::launch_evict(score, lens, src, dst, row_bytes, arrays, score_out, index, lens_out, B, Hkv, T, Tcap, Tcap_out, keep, recent,
                                     static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SB_OK : SB_ERR_LAUNCH;
