@@ -173,6 +173,7 @@ decode_kv4_kernel(const Args a)
     using P = Place<D, R>;
     constexpr int SHARES = NW * GMAX * CH * 16;
     __shared__ __attribute__((aligned(1024))) char smem[NW * P::BYTES > SHARES ? NW * P::BYTES : SHARES];
+    __shared__ __attribute__((aligned(16))) float was[FAR ? 4 : KEYS];   // scores of the round's keys, every wave its own
     f32x4* const ored = reinterpret_cast<f32x4*>(smem);                  // once the keys are done
 
     const int bkv = FAR ? blockIdx.y : blockIdx.x;     // entry * Hkv + kv head
@@ -227,7 +228,13 @@ decode_kv4_kernel(const Args a)
     };
     auto first_row_of = [&](int top) __attribute__((always_inline)) { return top - KW * R * (wave + 1); };
     auto fetch_k = [&](int top) __attribute__((always_inline)) { fetch(kc, ks, mem, mem + P::KS, first_row_of(top)); };
-    auto fetch_v = [&](int top) __attribute__((always_inline)) { fetch(vc, vs, mem + P::V, mem + P::VS, first_row_of(top)); };
+    const bool adds = !FAR && a.score && !a.wl;            // to scores, that come the same way, behind V
+    const uint64_t sc = adds ? scalar_base(reinterpret_cast<const uint8_t*>(a.score + (long)bkv * a.Tcap)) : 0;
+    const uint32_t scores = lds_offset(reinterpret_cast<const char*>(was)) + wave * R * KW * 4;
+    auto fetch_v = [&](int top) __attribute__((always_inline)) {
+        fetch(vc, vs, mem + P::V, mem + P::VS, first_row_of(top));
+        if (!FAR && adds && lane < R * KW / 4) dma16<FAR>(sc + (int64_t)first_row_of(top) * 4, max(4 * lane, lo - first_row_of(top)) * 4, scores);
+    };
     // where this lane's words are, in a wave's lowest tile (keys ascending: tile j of this wave is R - 1 - j tiles on)
     auto place = [&](int row, int byte) __attribute__((always_inline)) {
         return (row ^ P::x_of(row)) * P::ROW + (((byte >> 4) ^ P::y_of(row)) << 4 | (byte & 15));
@@ -249,7 +256,9 @@ decode_kv4_kernel(const Args a)
     auto round = [&]() __attribute__((always_inline)) {
         const bool more = hi - KEYS > lo;
         // ---- logits of the lane's eight keys, in base 2
-        dma_wait<P::LOADS>();              // K has landed, V was asked for behind it
+        // K has landed, V was asked for behind it
+        if (!FAR && adds) dma_wait<P::LOADS + 1>();
+        else dma_wait<P::LOADS>();
         float x[8];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
@@ -378,8 +387,7 @@ decode_kv4_kernel(const Args a)
                 acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, wb), acc[e], 0, 0, 0);
             }
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more) fetch_v(hi - KEYS);
+        // (stores go ahead of the next round's loads of V: what waits for K waits for nothing behind them)
         if (a.score_out) {
             if (a.wl) {
                 const int base = hi - KW * (mine + 1);
@@ -399,21 +407,24 @@ decode_kv4_kernel(const Args a)
                 const int base = hi - KW * (mine + 1), key = base + 8 * lq;
                 if (first && hc == 0 && base >= lo) {
                     const long at = (long)bkv * a.Tcap + key;
+                    const uint32_t mine_was = scores + ((R - 1 - mytile) * KW + 8 * lq) * 4;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (key + 4 * h + 4 <= len) {
                             f32x4 x = {w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]};
-                            if (a.score) x += *reinterpret_cast<const f32x4*>(a.score + at + 4 * h);
+                            if (adds) x += __builtin_bit_cast(f32x4, lds_load16(mine_was + 16 * h));
                             *reinterpret_cast<f32x4*>(a.score_out + at + 4 * h) = x;
                         } else {
 #pragma unroll
                             for (int r = 4 * h; r < 4 * h + 4; ++r)
-                                if (key + r < len) a.score_out[at + r] = (a.score ? a.score[at + r] : 0.0f) + w[r];
+                                if (key + r < len) a.score_out[at + r] = (adds ? lds_read<float>(mine_was + 4 * r) : 0.0f) + w[r];
                         }
                     }
                 }
             }
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) fetch_v(hi - KEYS);
         hi -= KEYS;
         par ^= 1;
         return more && (FAR || a.m || __builtin_amdgcn_ballot_w64(!(stick < LEAST)) != 0);
