@@ -227,7 +227,19 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
         return;
     }
     if constexpr (WHAT == 2) {
-        for (int c = a.chunks - 1; c > chunk; --c) stick *= left[c * 32];
+        // what the nearer chunks left: every second one a half-wave's, eight loads at once
+        constexpr int EACH = 8;
+        float mine = 1.0f;
+        for (int c = a.chunks - 1 - hh; c > chunk; c -= 2 * EACH) {
+            float x[EACH];
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) x[i] = left[max(c - 2 * i, chunk + 1) * 32];
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) mine *= c - 2 * i > chunk ? x[i] : 1.0f;
+        }
+        float lo_half, hi_half;
+        both_halves(mine, lo_half, hi_half);
+        stick *= lo_half * hi_half;
         const int done = none_left(stick) ? -1 : 0;
         if (lane == 0) s_done[0][wave] = done;
         barrier_lds();
