@@ -226,6 +226,12 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
         if (WHAT != 1 && tid == 0) reach[0] = reach[1] = 0;
         return;
     }
+    {
+        int qoff[C::LOADS];
+        sub_offsets<D>(qoff, lane);
+        const int r0 = min(32 * u.strip, (a.Tq - 1) / 32 * 32);
+        sub_to_lds<D>(a.q + (((long)b * a.H + u.head) * a.Tq + r0) * D, qoff, a.Tq - 1 - r0, tiles + wave * C::SUB, lane);
+    }
     if constexpr (WHAT == 2) {
         // what the nearer chunks left: every second one a half-wave's, eight loads at once
         constexpr int EACH = 8;
@@ -245,6 +251,7 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
         barrier_lds();
         if (waves_done(s_done[0])) {
             if (tid == 0) reach[0] = reach[1] = 0;
+            dma_wait<0>();
             return;
         }
     }
@@ -253,10 +260,6 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     const uint32_t smem0 = lds_offset(tiles);
     bf16x8 qf[D / 16];
     {
-        int qoff[C::LOADS];
-        sub_offsets<D>(qoff, lane);
-        const int r0 = min(32 * u.strip, (a.Tq - 1) / 32 * 32);
-        sub_to_lds<D>(a.q + (((long)b * a.H + u.head) * a.Tq + r0) * D, qoff, a.Tq - 1 - r0, tiles + wave * C::SUB, lane);
         dma_wait<0>();
         read_q<D>(qf, smem0 + wave * C::SUB, n, hh, u.there);
         barrier_lds();
