@@ -21,7 +21,7 @@ namespace {
 constexpr int NW = 4;                  // waves of a workgroup, a unit each
 constexpr int SNW = 8;                 // waves of a small kernel's workgroup
 constexpr int TK = 64;                 // keys of a tile
-constexpr int SUM_THREADS = 512;
+constexpr int SUM_DEEP = 4;            // groups that a wave of the last launch asks for at once
 
 template <int CTRL> __device__ __forceinline__ float dpp(float x)
 {
@@ -427,10 +427,10 @@ key_weight_small_kernel(const Args a)
 }
 
 // Groups by wave in turn, 64 keys a workgroup: a wave asks for four groups' numbers at a time, and how far a group reaches is the same for all its lanes.
-__global__ void __launch_bounds__(SUM_THREADS)
+template <int WAVES>
+__global__ void __launch_bounds__(64 * WAVES)
 key_weight_sum_kernel(const Args a)
 {
-    constexpr int WAVES = SUM_THREADS / 64, DEEP = 4;
     __shared__ float sums[WAVES][64];
     const int bkv = blockIdx.y, lane = threadIdx.x & 63, key = blockIdx.x * 64 + lane;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -439,18 +439,18 @@ key_weight_sum_kernel(const Args a)
     const float* part = a.part + (long)bkv * a.groups * a.Tpad + key;
     const int2* reach = reinterpret_cast<const int2*>(a.reach) + (long)bkv * a.groups * a.chunks + blockIdx.x * 64 / a.C;
     float s = 0.0f;
-    for (int g0 = wave; g0 < a.groups; g0 += DEEP * WAVES) {
-        int2 r[DEEP];
-        float x[DEEP];
+    for (int g0 = wave; g0 < a.groups; g0 += SUM_DEEP * WAVES) {
+        int2 r[SUM_DEEP];
+        float x[SUM_DEEP];
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) r[i] = reach[(long)min(g0 + i * WAVES, a.groups - 1) * a.chunks];
+        for (int i = 0; i < SUM_DEEP; ++i) r[i] = reach[(long)min(g0 + i * WAVES, a.groups - 1) * a.chunks];
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) {
+        for (int i = 0; i < SUM_DEEP; ++i) {
             x[i] = 0.0f;
             if (g0 + i * WAVES < a.groups && key >= r[i].x && key < r[i].y) x[i] = part[(long)(g0 + i * WAVES) * a.Tpad];
         }
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) s += x[i];
+        for (int i = 0; i < SUM_DEEP; ++i) s += x[i];
     }
     sums[wave][lane] = s;
     __syncthreads();
@@ -531,7 +531,13 @@ hipError_t launch_key_weight(const uint16_t* q, const uint16_t* k, const int* le
     a.reach = reinterpret_cast<int*>(a.left + (p.chunks > 1 ? (size_t)BHkv * p.units() * p.chunks * 32 : 0));
     const hipError_t e = d == 32 ? launch_d<32>(a, p, BHkv, stream) : d == 64 ? launch_d<64>(a, p, BHkv, stream) : launch_d<128>(a, p, BHkv, stream);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(key_weight_sum_kernel, dim3((unsigned)((T + 63) / 64), (unsigned)BHkv), dim3(SUM_THREADS), 0, stream, a);
+    // no more waves than have a group to add (B4 H16 T8192 d64, 128 rows, 4 groups: 9 us in all with one wave, 15.5 with eight)
+    auto sum = [&](auto kernel, int waves) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((T + 63) / 64), (unsigned)BHkv), dim3(64 * waves), 0, stream, a);
+    };
+    if (p.groups <= SUM_DEEP) sum(key_weight_sum_kernel<1>, 1);
+    else if (p.groups <= 2 * SUM_DEEP) sum(key_weight_sum_kernel<2>, 2);
+    else sum(key_weight_sum_kernel<8>, 8);
     return hipGetLastError();
 }
 
