@@ -8,9 +8,14 @@
 // In place of A V the sum of A over the queries.  A unit is 32 query rows of one head; units of the heads of a group at the
 // same rows are neighbours, as they read the same keys.  What a workgroup's queries give the keys, one number a key, goes into
 // the workspace, with how far it reaches; a last launch adds the workgroups up in a fixed order.
-//   key_weight_kernel        NW units a workgroup, 64-key tiles through LDS for all of them, from the last unit's diagonal towards key 0
-//   key_weight_small_kernel  one unit a workgroup, its waves 32 keys each, side by side; where there are few units, also split over
-//                            chunks of keys: a first launch finds what each chunk leaves of the sticks, a second one the weights
+//   key_weight_kernel        a unit a wave, or two where there are plenty; 64-key tiles through LDS for all of a workgroup, from the last unit's diagonal towards
+//                            key 0.  Few units at many keys are also split over chunks of keys: a first launch finds what each chunk leaves of the sticks, a
+//                            second one the weights
+//   key_weight_small_kernel  one unit a workgroup, its waves 32 keys each, side by side
+// Bound by vector instructions: 16 exponentials a lane and 32 keys, which alone are a third of the time, and some 110 others, at 40 million subtiles of 32 x 32 an
+// ms: B1 H32 Hkv8 T8192 d128, all far, 401 us (its products alone 27 us, its exponentials 110).  A third of the kv heads far 188, none 40.  Three and four tiles of K under
+// way instead of two, or two and four waves a unit, gain nothing here (402 -> 482 with four).
+#include <climits>
 #include <type_traits>
 #include "sb_kernels.h"
 #include "sb_mma.h"
@@ -69,12 +74,12 @@ __device__ __forceinline__ int length_of(const int* lens, int b, int most)
 constexpr float LEAST = 0x1p-126f;     // of the stick
 __device__ __forceinline__ bool none_left(float stick) { return __builtin_amdgcn_ballot_w64(!(stick < LEAST)) == 0; }
 
-// One query's share of N subtiles of 32 keys, the first the nearest, a half-wave 16 keys of each: with the stick whole before a subtile's nearest
-// key, the weight of key r is w[r] * mine, and `all` is what its 32 leave.  MASK: keys from `visible` (of the first; 32 i more of the others) on are
-// not seen.  (N = 2: one subtile's instructions fill the other's waits.)
+// One query's share of 32 keys, a half-wave 16 of them, N times (two subtiles of keys, or two queries): with the stick whole before a subtile's nearest
+// key, the weight of key r is w[r] * mine, and `all` is what its 32 leave.  MASK: keys from `visible` on are not seen.  (N = 2: one's instructions fill the
+// other's waits.)
 template <int N> using f32xn = float __attribute__((ext_vector_type(N)));
 template <bool MASK, int N>
-__device__ __forceinline__ void weights(const f32x16 (&s)[N], float c2, int visible, int hh, float (&w)[N][16], f32xn<N>& mine, f32xn<N>& all)
+__device__ __forceinline__ void weights(const f32x16 (&s)[N], float c2, const int (&visible)[N], int hh, float (&w)[N][16], f32xn<N>& mine, f32xn<N>& all)
 {
     // w[r] = W_r e_r, W_{r+1} = W_r + w[r], e = sigma / (1 - sigma): W_r = prod_{r' < r} 1 / (1 - sigma_r')
     float W[N], most = 0.0f;
@@ -85,7 +90,7 @@ __device__ __forceinline__ void weights(const f32x16 (&s)[N], float c2, int visi
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float e = fast_exp2(s[i][r] * c2);
-            if (MASK) e = r < visible + 32 * i ? e : 0.0f;
+            if (MASK) e = r < visible[i] ? e : 0.0f;
             w[i][r] = W[i] * e;
             W[i] += w[i][r];
         }
@@ -102,7 +107,7 @@ __device__ __forceinline__ void weights(const f32x16 (&s)[N], float c2, int visi
             float run = 0.0f;
 #pragma unroll
             for (int r = 15; r >= 0; --r) {
-                const float x = !MASK || r < visible + 32 * i ? s[i][r] * c2 : -INFINITY;
+                const float x = !MASK || r < visible[i] ? s[i][r] * c2 : -INFINITY;
                 run += sp2(x);
                 w[i][r] = fast_exp2(x - run);
             }
@@ -176,9 +181,10 @@ template <int D> __device__ __forceinline__ void read_q(bf16x8 (&qf)[D / 16], ui
     }
 }
 
-// of N subtiles at `at` and from there down
-template <int D, int N> __device__ __forceinline__ void logits(f32x16 (&s)[N], const bf16x8 (&qf)[D / 16], const uint32_t (&aoff)[D / 16], uint32_t at)
+// of N in all: NU units' with the subtiles of keys at `at` and from there down
+template <int D, int NU, int N> __device__ __forceinline__ void logits(f32x16 (&s)[N], const bf16x8 (&qf)[NU][D / 16], const uint32_t (&aoff)[D / 16], uint32_t at)
 {
+    static_assert(NU == 1 || NU == N, "one unit, or one subtile");
 #pragma unroll
     for (int j = 0; j < N; ++j)
 #pragma unroll
@@ -187,11 +193,13 @@ template <int D, int N> __device__ __forceinline__ void logits(f32x16 (&s)[N], c
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lds_load16(aoff[i] + at - j * Cfg<D>::SUB)), qf[i], s[j], 0, 0, 0);
+            s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lds_load16(aoff[i] + at - (NU == 1 ? j : 0) * Cfg<D>::SUB)), qf[NU == 1 ? 0 : j][i], s[j], 0, 0, 0);
 }
 
 // WHAT: 0 the weights of all keys, 1 what a chunk of keys leaves of the sticks, 2 the weights of a chunk
-template <int D, int WHAT>
+// NU: units of a wave.  One: it takes both halves of a tile at once.  Two: a half for both units, which read K once and add their weights up before they
+// are summed over the lanes (a unit's vector instructions are a fifth fewer, but a tile takes a workgroup longer).
+template <int D, int WHAT, int NU>
 __global__ void __launch_bounds__(64 * NW, 2)
 key_weight_kernel(const Args a, int BHkv, int first_wg)
 {
@@ -212,26 +220,36 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     const int n = lane & 31, hh = lane >> 5;
     const int len = length_of(a.lens, b, a.T), qlen = length_of(a.qlens, b, a.Tq);
     const int off = len - qlen;                                         // position of query row 0
-    const int unit = grp * NW + wave;
+    const int unit = (grp * NW + wave) * NU;
     int* const reach = a.reach + (((long)bkv * a.groups + grp) * a.chunks + chunk) * 2;
     float* const left = a.left + (((long)bkv * a.groups * NW + unit) * a.chunks) * 32 + n;       // of chunk 0
-    const Unit u = unit_of(a, unit, bkv, off, qlen, n);
-    const int last_strip = min((grp * NW + NW - 1) / a.G, (qlen - 1) / 32);            // of the workgroup, with rows in it
+    Unit u[NU];
+    f32xn<NU> stick;
+    int all_see = INT_MAX, some_see = 0;                                // (as Unit's)
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+        u[i] = unit_of(a, unit + i, bkv, off, qlen, n);
+        stick[i] = u[i].there ? 1.0f : 0.0f;
+        all_see = min(all_see, u[i].all);
+        some_see = max(some_see, u[i].some);
+    }
+    auto left_of = [&]() __attribute__((always_inline)) { return NU == 1 ? stick[0] : stick[0] + stick[NU - 1]; };
+    const int last_strip = min(((grp + 1) * NW * NU - 1) / a.G, (qlen - 1) / 32);            // of the workgroup, with rows in it
     const int lo = WHAT ? chunk * a.C : 0;
-    int top = grp * NW / a.G * 32 < qlen ? max(0, off + min(32 * last_strip + 32, qlen) - 1) : 0;
+    int top = grp * NW * NU / a.G * 32 < qlen ? max(0, off + min(32 * last_strip + 32, qlen) - 1) : 0;
     if (WHAT) top = min(top, lo + a.C);
-    float stick = u.there ? 1.0f : 0.0f;
     if (top <= lo) {
-        if (WHAT == 1 && hh == 0) left[chunk * 32] = stick;
+        if (WHAT == 1 && hh == 0) left[chunk * 32] = stick[0];
         if (WHAT != 1 && tid == 0) reach[0] = reach[1] = 0;
         return;
     }
-    {
-        int qoff[C::LOADS];
-        sub_offsets<D>(qoff, lane);
+    int qoff[C::LOADS];
+    sub_offsets<D>(qoff, lane);
+    auto fetch_q = [&](const Unit& u) __attribute__((always_inline)) {
         const int r0 = min(32 * u.strip, (a.Tq - 1) / 32 * 32);
         sub_to_lds<D>(a.q + (((long)b * a.H + u.head) * a.Tq + r0) * D, qoff, a.Tq - 1 - r0, tiles + wave * C::SUB, lane);
-    }
+    };
+    fetch_q(u[0]);
     if constexpr (WHAT == 2) {
         // what the nearer chunks left: every second one a half-wave's, eight loads at once
         constexpr int EACH = 8;
@@ -245,8 +263,8 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
         }
         float lo_half, hi_half;
         both_halves(mine, lo_half, hi_half);
-        stick *= lo_half * hi_half;
-        const int done = none_left(stick) ? -1 : 0;
+        stick[0] *= lo_half * hi_half;
+        const int done = none_left(stick[0]) ? -1 : 0;
         if (lane == 0) s_done[0][wave] = done;
         barrier_lds();
         if (waves_done(s_done[0])) {
@@ -258,12 +276,17 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
 
     const float c2 = SB_LOG2E / sqrtf((float)D);
     const uint32_t smem0 = lds_offset(tiles);
-    bf16x8 qf[D / 16];
-    {
+    bf16x8 qf[NU][D / 16];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+        if (i > 0) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the rows before have been read)
+            fetch_q(u[i]);
+        }
         dma_wait<0>();
-        read_q<D>(qf, smem0 + wave * C::SUB, n, hh, u.there);
-        barrier_lds();
+        read_q<D>(qf[i], smem0 + wave * C::SUB, n, hh, u[i].there);
     }
+    barrier_lds();
     const uint16_t* const kg = reinterpret_cast<const uint16_t*>(scalar_base(a.k + (long)bkv * a.Tcap * D));
     int goff[NPW];
 #pragma unroll
@@ -298,37 +321,48 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
             if (jt < jend || waves_done(s_done[par ^ 1])) return false;
         }
         if (jt > jend) stage(jt - 1, par ^ 1);
-        const int base = jt * TK + 32;                     // of the nearer subtile
-        float sum[2] = {0.0f, 0.0f};
-        if (base - 32 < u.some && !none_left(stick)) {
+        float sum[2] = {0.0f, 0.0f};                       // of the nearer half, of the farther
+#pragma unroll
+        for (int half = 0; half < NU; ++half) {            // (one unit: both at once)
+            const int base = jt * TK + 32 - 32 * half;
+            if ((NU == 1 ? base - 32 : base) >= some_see || none_left(left_of())) continue;
             f32x16 s[2];
-            logits<D>(s, qf, aoff, par * TILE + C::SUB);
             float w[2][16];
             f32xn<2> mine, all;
-            if (base + 32 > u.all) weights<true>(s, c2, u.sees - base - 16 * hh, hh, w, mine, all);
-            else weights<false>(s, c2, 0, hh, w, mine, all);
+            logits<D, NU>(s, qf, aoff, par * TILE + (1 - half) * C::SUB);
+            const int seen[2] = {u[0].sees - base - 16 * hh, (NU == 1 ? u[0].sees + 32 : u[NU - 1].sees) - base - 16 * hh};
+            if (base + 32 > all_see) weights<true>(s, c2, seen, hh, w, mine, all);
+            else weights<false>(s, c2, seen, hh, w, mine, all);
+            if constexpr (NU == 1) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if constexpr (WHAT != 1) {
-                    mine[i] *= stick;
+                for (int i = 0; i < 2; ++i) {
+                    if constexpr (WHAT != 1) {
+                        mine[i] *= stick[0];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) w[i][r] *= mine[i];
-                    sum[i] = sums_of_lanes(w[i], n);
+                        for (int r = 0; r < 16; ++r) w[i][r] *= mine[i];
+                        sum[i] = sums_of_lanes(w[i], n);
+                    }
+                    stick[0] *= all[i];
                 }
-                stick *= all[i];
+            } else {
+                mine *= stick;
+                stick *= all;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) w[0][r] = w[0][r] * mine[0] + w[1][r] * mine[1];
+                sum[half] = sums_of_lanes(w[0], n);
             }
         }
         if (WHAT != 1 && (n & 1) == 0) {
             csum[par][wave][32 + 16 * hh + key_of_lane(n)] = sum[0];
             csum[par][wave][16 * hh + key_of_lane(n)] = sum[1];
         }
-        const int done = none_left(stick) ? -1 : 0;
+        const int done = none_left(left_of()) ? -1 : 0;
         if (lane == 0) s_done[par][wave] = done;
         --jt;
         return true;
     };
     while (tile(std::integral_constant<int, 0>()) && tile(std::integral_constant<int, 1>())) {}
-    if (WHAT == 1 && hh == 0) left[chunk * 32] = stick;
+    if (WHAT == 1 && hh == 0) left[chunk * 32] = stick[0];
     if (WHAT != 1 && tid == 0) {
         reach[0] = (jt + 1) * TK;
         reach[1] = (jt0 + 1) * TK;
@@ -380,22 +414,22 @@ key_weight_small_kernel(const Args a)
     for (int s = 0; s < D / 16; ++s) aoff[s] = lds_offset(mine_at) + tile_off_perm<D>(perm_row(n), 2 * s + hh);
     dma_wait<C::LOADS>();
     barrier_lds();
-    bf16x8 qf[D / 16];
-    read_q<D>(qf, lds_offset(qrows), n, hh, u.there);
+    bf16x8 qf[1][D / 16];
+    read_q<D>(qf[0], lds_offset(qrows), n, hh, u.there);
 
     float* const part = a.part + ((long)bkv * a.groups + unit) * a.Tpad;
     for (int par = 0; hi > 0; par ^= 1) {
         const int base = hi - 32 * (wave + 1);
         dma_wait<0>();
         f32x16 s[1];
-        logits<D>(s, qf, aoff, 0);
+        logits<D, 1>(s, qf, aoff, 0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the rows have been read)
         if (hi > 32 * SNW) fetch(base - 32 * SNW);
         float w[1][16];
         f32xn<1> mine = 0.0f, all = 1.0f;
         if (base >= 0) {
-            if (base + 32 > u.all) weights<true>(s, c2, u.sees - base - 16 * hh, hh, w, mine, all);
-            else weights<false>(s, c2, 0, hh, w, mine, all);
+            if (base + 32 > u.all) weights<true>(s, c2, {u.sees - base - 16 * hh}, hh, w, mine, all);
+            else weights<false>(s, c2, {0}, hh, w, mine, all);
         } else {
 #pragma unroll
             for (int r = 0; r < 16; ++r) w[0][r] = 0.0f;
@@ -464,7 +498,7 @@ key_weight_sum_kernel(const Args a)
 }
 
 struct Plan {
-    bool small;
+    bool small, pairs;
     int groups, chunks, C;
     int Tpad;
     int units() const { return small ? groups : groups * NW; }
@@ -474,14 +508,17 @@ struct Plan {
 // units fit the chip, 256 of them at a time beyond.  Four units: 1.4 for a tile of 64 keys of the longest, or 0.45 ns a subtile of all, whichever is more.  Chunks of
 // keys in two launches: 8 more, 0.8 ns a subtile.  Measured with all heads far, one unit / four units / chunks (768 workgroups):
 //   B4 H12 Hkv4 T2048 d128, whole prompt 73 / 52;  B8 H16 T2048 d64 156 / 95;  B1 H12 Hkv4 T3000 d64 36 / 55 / 59;  B1 H4 T4000 d128 38 / 84 / 50;
-//   B2 H16 Hkv8 T700 d128 16.5 / 19 / 19;  64 rows of B1 H32 Hkv8 T16384 d128 - / 309 / 39;  one row of B1 H32 Hkv8 T4000 d128 27 / 80 / 17
+//   B2 H16 Hkv8 T700 d128 16.5 / 19 / 19;  64 rows of B1 H32 Hkv8 T16384 d128 - / 309 / 38;  one row of B1 H32 Hkv8 T4000 d128 27 / 80 / 16
+// Two units a wave where the longest workgroup's tiles, 2.1 each, take no longer than all the work does with a third of the kv heads far.  One / two, a third
+// far, then all:  B16 H16 T2048 d32 102 / 87, 173 / 138;  B2 H64 Hkv8 T4096 d64 139 / 133, 328 / 279;  B8 H32 Hkv8 T2048 d128 113 / 111, 231 / 211;
+//   B8 H16 T4096 d64 167 / 175, 347 / 302;  not B8 H16 T2048 d64 63 / 64, 98 / 86;  B1 H32 Hkv8 T8192 d128 199 / 264, 417 / 414
 Plan plan_of(int B, int H, int Hkv, int Tq, int T)
 {
     const int G = H / Hkv, units = (Tq + 31) / 32 * G, Tpad = (T + TK - 1) / TK * TK;
     const double all = (double)B * Hkv * units, mean = (T - 0.5 * Tq) / T;            // share of the keys that a query sees in the mean
     const double subtiles = all * mean * T / 32.0;
     const double small = 1.25 * (T / 256 + 1) * std::max(1.0, all * mean / 256.0);
-    Plan p = {false, (units + NW - 1) / NW, 1, Tpad, Tpad};
+    Plan p = {false, false, (units + NW - 1) / NW, 1, Tpad, Tpad};
     const long wgs = (long)B * Hkv * p.groups;
     const int tiles = Tpad / TK;
     const int want = (int)std::max(1L, std::min<long>(tiles / 2, 768 / wgs));
@@ -492,6 +529,9 @@ Plan plan_of(int B, int H, int Hkv, int Tq, int T)
         p.C = (tiles + want - 1) / want * TK;
         p.chunks = (T + p.C - 1) / p.C;
         if (p.chunks == 1) p.C = Tpad;
+    } else if (2.1 * tiles <= 0.00015 * subtiles) {
+        p.pairs = true;
+        p.groups = (units + 2 * NW - 1) / (2 * NW);
     }
     return p;
 }
@@ -504,13 +544,14 @@ template <int D> hipError_t launch_d(const Args& a, const Plan& p, int BHkv, hip
     }
     if (a.chunks == 1)
         return launch_workgroups((long)BHkv * a.groups, 64 * NW, [&](unsigned wgs, int first) {
-            hipLaunchKernelGGL((key_weight_kernel<D, 0>), dim3(wgs), dim3(64 * NW), 0, stream, a, BHkv, first);
+            if (p.pairs) hipLaunchKernelGGL((key_weight_kernel<D, 0, 2>), dim3(wgs), dim3(64 * NW), 0, stream, a, BHkv, first);
+            else hipLaunchKernelGGL((key_weight_kernel<D, 0, 1>), dim3(wgs), dim3(64 * NW), 0, stream, a, BHkv, first);
         });
     const dim3 grid((unsigned)(BHkv * a.groups), (unsigned)a.chunks), threads(64 * NW);
-    hipLaunchKernelGGL((key_weight_kernel<D, 1>), grid, threads, 0, stream, a, BHkv, 0);
+    hipLaunchKernelGGL((key_weight_kernel<D, 1, 1>), grid, threads, 0, stream, a, BHkv, 0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((key_weight_kernel<D, 2>), grid, threads, 0, stream, a, BHkv, 0);
+    hipLaunchKernelGGL((key_weight_kernel<D, 2, 1>), grid, threads, 0, stream, a, BHkv, 0);
     return hipGetLastError();
 }
 

@@ -207,3 +207,42 @@ def test_store_goes_to_its_stream(sb):
     torch.cuda.synchronize()
     for a, b in zip(cache, want):
         assert torch.equal(a, b)
+
+
+# Two units a wave where the work of all, by the keys that a query sees, is some 7000 whole units of 32 query rows (more where the last 64 keys are few).  Groups whose heads end inside a pair, an odd number of strips,
+# windows, padded entries; and fewer units beside them
+@pytest.mark.parametrize("B,H,Hkv,Tq,T,d", [(128, 96, 32, 70, 70, 32), (70, 96, 96, 95, 95, 64), (48, 32, 8, 300, 300, 128), (52, 30, 2, 300, 333, 64), (128, 64, 16, 33, 200, 128),
+                                              (9, 32, 8, 300, 300, 128)])
+def test_key_weights_of_many_units(sb, oracle, B, H, Hkv, Tq, T, d):
+    """Every entry as a call of its own gives it (which is held against the oracle elsewhere), and some against the oracle.  A weight is off by
+    rel = (T + 64) 2^-23 + 8 dz of it, dz what d products and sums in fp32 are off in a logit of the largest q and k; a key's sum by that share of itself,
+    and by a rounding of half a step for each of its Tq G terms: once against the oracle, twice between two calls."""
+    g = torch.Generator().manual_seed(B + T)
+    G, far = H // Hkv, (6.0 * d ** 0.5) ** 0.5
+    q, k = torch.randn(B, H, Tq, d, generator=g), torch.randn(B, Hkv, T, d, generator=g)
+    k[:, 1::2, :, d - 1] = -far
+    q.view(B, Hkv, G, Tq, d)[:, 1::2, ..., d - 1] = far
+    q, k = q.bfloat16(), k.bfloat16()
+    lens, qlens = [T] * B, [Tq] * B
+    lens[1], lens[2], lens[3], lens[B - 1] = 0, 1, T // 2, T - 3
+    qlens[1], qlens[2], qlens[3], qlens[4] = 0, 1, min(Tq, T // 2), Tq - 1
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    qd, kd = q.cuda(), k.cuda()
+    for b in range(B):                                   # padding is anything at all
+        kd[b, :, lens[b]:], qd[b, :, qlens[b]:] = float("nan"), float("nan")
+    was = torch.rand(B, Hkv, T, generator=g).cuda()
+    got = sb.sb_attn_key_weight(qd, kd, lens=ints(lens), qlens=ints(qlens), score=was, score_out=torch.full_like(was, -7.0))
+    dz = d * U * float(q.abs().max()) * float(k.abs().float().sum(-1).max()) / d ** 0.5 / 4
+    rel = (T + 64) * 2 * U + 8 * dz
+    bound = lambda want, ref: rel * (1.0 + want) + (Tq * G + 2) * U * ref
+    for b in range(B):
+        n = lens[b]
+        one = sb.sb_attn_key_weight(qd[b:b + 1].clone(), kd[b:b + 1].clone(), lens=ints(lens[b:b + 1]), qlens=ints(qlens[b:b + 1]), score=was[b:b + 1].clone(), score_out=torch.empty_like(was[b:b + 1]))
+        a, c, w = to64(got[b, :, :n]), to64(one[0, :, :n]), to64(was[b, :, :n])
+        assert (np.abs(a - c) <= 2 * bound(c - w, c)).all(), b
+        assert (got[b, :, n:] == -7.0).all()
+    for b in (0, 1, 2, 3, 4, B - 1):
+        n, m = lens[b], qlens[b]
+        want = oracle.key_weight(to64(q)[b:b + 1, :, :m], to64(k)[b:b + 1, :, :n])[0]
+        ref = want + to64(was)[b, :, :n]
+        assert (np.abs(to64(got)[b, :, :n] - ref) <= bound(want, ref)).all(), b
