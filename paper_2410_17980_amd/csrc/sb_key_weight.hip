@@ -12,9 +12,9 @@
 //                            key 0.  Few units at many keys are also split over chunks of keys: a first launch finds what each chunk leaves of the sticks, a
 //                            second one the weights
 //   key_weight_small_kernel  one unit a workgroup, its waves 32 keys each, side by side
-// Bound by vector instructions: 16 exponentials a lane and 32 keys, which alone are a third of the time, and some 110 others, at 40 million subtiles of 32 x 32 an
-// ms: B1 H32 Hkv8 T8192 d128, all far, 401 us (its products alone 27 us, its exponentials 110).  A third of the kv heads far 188, none 40.  Three and four tiles of K under
-// way instead of two, or two and four waves a unit, gain nothing here (402 -> 482 with four).
+// Bound by vector instructions: for 32 x 32 weights 16 exponentials a lane and some 110 others, next to the D / 16 matrix products.  B1 H32 Hkv8 T8192 d128,
+// 1.05 million such squares, all far 401 us, a third of the kv heads 188, none 40; the products alone are 216 us at the 1271 TFLOP/s that a product of 8192^3 reaches
+// here (109 at the chip's peak), the exponentials alone 109 at 2.4 GHz.  Three and four tiles of K under way instead of two, or four waves a unit, gain nothing (402 -> 482 with four).
 #include <climits>
 #include <type_traits>
 #include "sb_kernels.h"
