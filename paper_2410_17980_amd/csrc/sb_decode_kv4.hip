@@ -65,6 +65,15 @@ __device__ __forceinline__ int length_of(const Args& a, int b)
 }
 __device__ __forceinline__ int up32(int n) { return (n + 31) & ~31; }
 
+// The entry and kv head of a near workgroup.  A CU gets workgroups i, i + 256, ..: with 16 kv heads, the same head of several entries, and heads that reach far would come
+// together.  So the heads of an entry turn by one for each 256 workgroups in front of it (B32 H16 T1800 d64, a third of the heads far, 18.2 -> 15.4 us, d128 23.7 -> 20.5; none
+// far 6.7 -> 6.7, at d = 32 6.0 -> 6.4).
+__device__ __forceinline__ int turned(int wg, int Hkv)
+{
+    const int first = wg / Hkv * Hkv;
+    return first < 256 ? wg : first + (wg - first + first / 256) % Hkv;
+}
+
 template <int CTRL> __device__ __forceinline__ float dpp(float x)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
@@ -176,12 +185,12 @@ decode_kv4_kernel(const Args a)
     __shared__ __attribute__((aligned(16))) float was[FAR ? 4 : KEYS];   // scores of the round's keys, every wave its own
     f32x4* const ored = reinterpret_cast<f32x4*>(smem);                  // once the keys are done
 
-    const int bkv = FAR ? blockIdx.y : blockIdx.x;     // entry * Hkv + kv head
+    const int bkv = FAR ? (int)blockIdx.y : turned((int)blockIdx.x, a.Hkv);      // entry * Hkv + kv head
     const int g0 = blockIdx.z * GMAX;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, lq = lane >> 4;
-    const int b = bkv / a.Hkv;
+    const int b = (int)(FAR ? blockIdx.y : blockIdx.x) / a.Hkv;
     const int len = length_of(a, b), end = up32(len);
     const int slot = FAR ? (int)blockIdx.x + (a.near > 0) : 0;
     const int top = FAR ? end - a.near - (int)blockIdx.x * a.C : end;
