@@ -613,16 +613,18 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
 constexpr long round_of(int d) { return d == 128 ? 256 : 512; }
 
 // The cache is the near launch's alone where its rounds (1.4 us each at d = 128, 1.0 below, as long as all its workgroups run at once) take no
-// longer than the two other launches.  Alone / three launches, us, no head far, then a third of the kv heads, then all:
-//   d = 128  B16 H8 T2800 5.8 / 10.1, 19.8 / 16.0, 20.4 / 21.6;  not T4000 5.2 / 10.0, 27.3 / 16.7, 27.7 / 25.8;  B32 H16 T2800 8.5 / 13.9, 32.7 / 31.5, 39.3 / 45.3;
-//            not T4000 8.5 / 13.9, 46 / 37, 55 / 58;  of more than two rounds of workgroups B32 H32 T1300 14.1 / 16.1, 35.5 / 34.5, 43 / 48;  not T2000 14.4 / 16.6, 46 / 39, 58 / 61
-//   d = 64   B32 H16 T2800 6.7 / 13.6, 23.1 / 23.7, 26.4 / 32.1;  not B16 H8 T4000 5.6 / 13.4, 23.0 / 15.3, 23.1 / 19.4, B32 H32 T4000 8.6 / 14.5, 49 / 40, 59 / 64
-//   d = 32   B32 H16 T2800 5.7 / 10.0, 21.3 / 19.5, 22.5 / 25.2;  not T4000 5.6 / 9.9, 29.6 / 21.8, 30.9 / 28.7
+// longer than the two other launches; beyond one workgroup a CU near and far heads share the CUs, and what a launch in front costs weighs more.
+// Alone / three launches, us, no head far, then a third of the kv heads, then all:
+//   256 workgroups at most  d = 128 B16 H8 T2800 5.8 / 10.1, 19.8 / 16.0, 20.4 / 21.6;  not T4000 5.2 / 10.0, 27.3 / 16.7, 27.7 / 25.8;  d = 64 not T4000 5.6 / 13.4, 23.0 / 15.3, 23.1 / 19.4
+//   more  d = 128  B20 H16 T4000 7.6 / 13.3, 33 / 36, 42 / 42;  B32 H16 T4000 8.5 / 13.9, 34 / 36, 54 / 58, not T6500 8.5 / 14.1, 51 / 50, 85 / 84;  B32 H32 T2000 14.7 / 17.2, 37 / 40, 55 / 60,
+//                  T4000 14.4 / 17.5, 58 / 58, 105 / 100;  B64 H32 T4000 27 / 24, 97 / 135, 194 / 187
+//         d = 64   B20 H16 T4000 6.6 / 12.9, 25 / 27, 35 / 29;  B32 H16 T4000 6.9 / 13.4, 26 / 26, 38 / 39, not T6500 6.8 / 13.5, 42 / 36, 59 / 53;  B64 H32 T5000 14.2 / 18.4, 65 / 108, 133 / 132
+//         d = 32   B32 H16 T4000 6.4 / 12.3, 25 / 23, 32 / 29;  B32 H32 T4000 7.0 / 13.9, 28 / 32, 41 / 44
 // Where m is wanted every key is read anyway, alone / spread (below): d = 128 B4 H8 T700 7.8 / 7.9, B32 H16 T2000 29.7 / 30.6;  not B4 H8 T1300 12.3 / 8.1, B16 H8 T1300 12.5 / 11.0
-inline int alone_up_to(long wgs, int d, bool want_m)
+inline int alone_up_to(long wgs, bool want_m)
 {
     if (want_m) return wgs <= 256 ? 4 * NEAR : 8 * NEAR;
-    return d == 128 && wgs > 2 * round_of(d) ? 6 * NEAR : 13 * NEAR;
+    return wgs <= 256 ? 13 * NEAR : 16 * NEAR;
 }
 
 // A small cache is spread over the chip, every key read, in two launches: 8 us and 0.16 us per MB beyond 6.  The limits lie where what is lost where no head is
@@ -645,7 +647,7 @@ struct Split {
 Split split_of(long wgs, double cache_bytes, int T, int d, bool want_m)
 {
     const bool spread = !want_m && spread_small(cache_bytes, T, d);
-    if (T <= alone_up_to(wgs, d, want_m) && !spread) return {(T + 31) & ~31, KW * FAR_NW, 1};
+    if (T <= alone_up_to(wgs, want_m) && !spread) return {(T + 31) & ~31, KW * FAR_NW, 1};
     Split s = {want_m || spread ? 0 : NEAR, 0, 0};
     constexpr int unit = 2 * KW * FAR_NW;
     const int far = T + KW - 1 - s.near;

@@ -37,7 +37,7 @@ def activations(B, H, Hkv, T, d, seed):
 # d = 64 and 32 from 513; up to four query heads a kv head; short caches, ends inside a round, and such that need the far launch as well
 @pytest.mark.parametrize("want_m", [False, True])
 @pytest.mark.parametrize("B,H,Hkv,T,d", [(37, 8, 8, 200, 128), (37, 16, 8, 1000, 128), (33, 32, 8, 300, 128), (70, 8, 8, 33, 64), (65, 32, 8, 1500, 32), (33, 8, 8, 3500, 128),
-                                         (33, 40, 8, 300, 128), (66, 16, 8, 3600, 64)])
+                                         (33, 40, 8, 300, 128), (66, 16, 8, 3600, 64), (33, 16, 16, 4200, 32), (33, 8, 8, 4200, 64)])
 def test_decode_of_many_heads(sb, oracle, B, H, Hkv, T, d, want_m):
     """Against the oracle for a sample of entries, in the bounds of the 4-bit decode's tests: a weight is off by rel = (T + 64) 2^-23 + 8 dz of it,
     o by that, by 2^-16 of the largest value, and by half a step (2^-8); and every entry as it comes out of a call of its own."""
