@@ -246,3 +246,76 @@ def test_key_weights_of_many_units(sb, oracle, B, H, Hkv, Tq, T, d):
         want = oracle.key_weight(to64(q)[b:b + 1, :, :m], to64(k)[b:b + 1, :, :n])[0]
         ref = want + to64(was)[b, :, :n]
         assert (np.abs(to64(got)[b, :, :n] - ref) <= bound(want, ref)).all(), b
+
+
+@pytest.mark.parametrize("T", [131_073, 524_288])
+@pytest.mark.parametrize("want_m", [False, True])
+def test_decode_of_the_longest_caches(sb, oracle, T, want_m):
+    """Logits around -12, so that the last of 524288 keys still counts.  Bounds as in test_decode_of_many_heads."""
+    B, H, Hkv, d = 1, 4, 2, 32
+    g = torch.Generator().manual_seed(T)
+    q, k, v = torch.randn(B, H, d, generator=g), torch.randn(B, Hkv, T, d, generator=g), torch.randn(B, Hkv, T, d, generator=g)
+    k[:, 1, :, d - 1], q[:, 2:, d - 1] = -8.0, 12.0 * d ** 0.5 / 8.0
+    q, k, v = (t.bfloat16().cuda() for t in (q, k, v))
+    cap = (T + 31) // 32 * 32
+    cache = new_cache(B, Hkv, cap, d)
+    sb.sb_attn_kv4_store(k, v, *cache)
+    k4, v4 = (to64(t)[0] for t in sb.sb_attn_kv4_load(*cache, T))
+    got = sb.sb_attn_decode_kv4(q, *cache, T=T, score_out=torch.zeros(B, Hkv, cap, device="cuda"), want_m=want_m)
+    for h in range(Hkv):
+        total, rel = np.zeros(T), 0.0
+        for i in (2 * h, 2 * h + 1):
+            qi = to64(q)[0, i]
+            A, left = oracle.row_weights(qi, k4[h])
+            dz = d * U * (np.abs(k4[h]) @ np.abs(qi)).max() / np.sqrt(d)
+            rel = max(rel, (T + 64) * 2 * U + 8 * dz)
+            want = A @ v4[h]
+            assert (np.abs(to64(got[0])[0, i] - want) <= 2.0 ** -8 * np.abs(want) + np.abs(v4[h]).max() * (2.0 ** -16 + rel)).all()
+            total += A
+        s = to64(got[-1])[0, h, :T]
+        assert (np.abs(s - total) <= 2 * rel * total + 6 * U * total + 1e-37).all()          # of each weight itself
+        assert h == 0 or total[0] > 1e-8
+
+
+@pytest.mark.parametrize("Tq", [1, 40])
+def test_key_weights_of_the_longest_caches(sb, oracle, Tq):
+    T, d = 524_288, 32
+    g = torch.Generator().manual_seed(Tq)
+    q, k = torch.randn(1, 1, Tq, d, generator=g), torch.randn(1, 1, T, d, generator=g)
+    k[..., d - 1], q[..., d - 1] = -8.0, 12.0 * d ** 0.5 / 8.0
+    q, k = q.bfloat16(), k.bfloat16()
+    got = to64(sb.sb_attn_key_weight(q.cuda(), k.cuda()))[0, 0]
+    want = oracle.key_weight(to64(q), to64(k))[0, 0]
+    dz = d * U * float(q.abs().float().max()) * float(k.abs().float().sum(-1).max()) / d ** 0.5
+    assert (np.abs(got - want) <= ((T + 64) * 2 * U + 8 * dz + (Tq + 2) * U) * want + 1e-37).all() and want[0] > 1e-8
+
+
+def test_entries_beyond_four_gigabytes(sb):
+    """The last of three entries of a cache of 2^25 rows, as the same rows in a small cache give it."""
+    big, small, n, d = 1 << 25, 2080, 2048, 64
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("not enough memory")
+    q, k, v = activations(1, 2, 1, n, d, seed=40)
+    part = new_cache(1, 1, small, d)
+    sb.sb_attn_kv4_store(k, v, *part)
+    cache = [torch.zeros(3, 1, big, t.shape[-1], dtype=torch.uint8, device="cuda") for t in part]
+    for a, b in zip(cache, part):
+        a[2, :, :small] = b[0]
+    lens = torch.tensor([0, 0, n], dtype=torch.int32, device="cuda")
+    q3 = q.expand(3, -1, -1).contiguous()
+    score = torch.zeros(3, 1, big, device="cuda")
+    o, s = sb.sb_attn_decode_kv4(q3, *cache, T=n, lens=lens, score=score)
+    o1, s1 = sb.sb_attn_decode_kv4(q, *part, T=n, score=torch.zeros(1, 1, small, device="cuda"))
+    assert torch.equal(o[2], o1[0]) and torch.equal(s[2, 0, :n], s1[0, 0, :n]) and not s[2, 0, n:].any() and not o[:2].any()
+    out, so, lo, ix = sb.sb_attn_evict(s, cache, 1000, recent=10, T=n, lens=lens, out=[torch.zeros(3, 1, 1024, t.shape[-1], dtype=torch.uint8, device="cuda") for t in cache])
+    out1, so1, _, ix1 = sb.sb_attn_evict(s1, part, 1000, recent=10, T=n)
+    assert lo.tolist() == [0, 0, 1000] and torch.equal(ix[2], ix1[0]) and torch.equal(so[2, 0, :1000], so1[0, 0, :1000])
+    assert all(torch.equal(a[2, 0, :1000], b[0, 0, :1000]) and not a[:2].any() for a, b in zip(out, out1))
+    del cache, score, s, out
+    kb = torch.zeros(3, 1, big, d, dtype=torch.bfloat16, device="cuda")
+    kb[2, :, :n] = k[0]
+    qs = torch.randn(1, 2, 100, d, generator=torch.Generator().manual_seed(41)).bfloat16().cuda()
+    w = sb.sb_attn_key_weight(qs.expand(3, -1, -1, -1).contiguous(), kb, T=n, lens=lens)
+    w1 = sb.sb_attn_key_weight(qs, k)
+    assert torch.allclose(w[2, 0, :n], w1[0, 0], rtol=1e-5, atol=1e-7)
