@@ -609,7 +609,7 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
     }
 }
 
-// Workgroups of the near launch that one round of the chip holds: eight waves of 146 registers and 67 KB, 109 and 34 KB, 86 and 18 KB.
+// Workgroups of the near launch that one round of the chip holds: eight waves of 146 registers and 68 KB, 112 and 35 KB, 89 and 19 KB.
 constexpr long round_of(int d) { return d == 128 ? 256 : 512; }
 
 // The cache is the near launch's alone where its rounds (1.4 us each at d = 128, 1.0 below, as long as all its workgroups run at once) take no
