@@ -267,7 +267,7 @@ int sb_attn_kv4_load(const void* kc, const void* ks, const void* vc, const void*
  * heads of kv head h of A[i], for the entry's rows i; others are left as they were.  score may be
  * NULL (zeros) and may be score_out itself, but not overlap it otherwise (SB_ERR_OVERLAP).  At most
  * 1024 query heads a kv head and B*H <= 8388607 with score_out (16777215 without).
- * The weights that meet V are rounded to 16 bits (o itself has 8); score gets them in fp32.  Rows of
+ * Weights have fp32's 24 bits, in o (which is rounded once, at its end) and in score.  Rows of
  * which less than 2^-126 of the stick is left count as zero, a NaN among them too, as long as m is not wanted.
  * workspace: sb_attn_decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, score_out != NULL) bytes.
  * Bit-reproducible, as sb_attn_decode.

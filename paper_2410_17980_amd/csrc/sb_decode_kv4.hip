@@ -24,9 +24,11 @@
 // has its logits, V's behind its output.  (Straight to registers it is 14 loads a tile, and 26 registers a tile to hold them: all heads far, B8 H16 T16384, d = 128, 64, 32:
 // 69, 52, 37 us, through LDS with the same rounds 65, 44, 36.)  A near launch of more workgroups than the chip holds takes half as many waves a workgroup, two tiles each:
 // B32 H16 T2000 d128 9.8 -> 8.5 us with no head far, 30.5 -> 24.6 with a third; smaller ones lose by it (B16 H8 T2000 d128 15.2 -> 17.8).
+// V meets a weight in three parts of eight bits, bf16 each: 24 bits, all that it has, as in sb_decode.hip.  (Two parts, 16 bits, took 1 to 3 % less: B8 H16 T16384 d128, all far,
+// 55.5 / 55.9 us, B32 H16 T1800 d64 19.4 / 20.0.)
 // The 16 columns of the MFMAs are more than most groups have heads.  Their copies of a head take a tile each (two with up to four heads, R), which
-// halves the vector instructions of the weights (four tiles gain nothing more), and the upper 8 bits of a weight or the 8 below (o gets 16 bits of a weight; o itself has
-// 8), which halves the MFMAs of the output; the columns of a head are added up at the end.
+// halves the vector instructions of the weights (four tiles gain nothing more), and the parts of a weight (PIECES of them), so that one MFMA does for a tile with up to four heads,
+// two with up to eight, three beyond; the columns of a head are added up at the end.
 #include "sb_kernels.h"
 #include "sb_kv4.h"
 #include "sb_mma.h"
@@ -74,6 +76,10 @@ __device__ __forceinline__ int turned(int wg, int Hkv)
 template <int CTRL> __device__ __forceinline__ float dpp(float x)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_word(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
 }
 // x += what CTRL's lanes have
 template <int CTRL> __device__ __forceinline__ void add_columns(float (&x)[8])
@@ -158,14 +164,23 @@ template <int N> __device__ __forceinline__ void lds_words(uint32_t (&w)[N], uin
     }
 }
 
+// the upper halves of two numbers' bits, each a bf16, in one word; what is left of the numbers in their place
+__device__ __forceinline__ uint32_t upper_halves(float& a, float& b)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, a), v = __builtin_bit_cast(uint32_t, b);
+    a -= __builtin_bit_cast(float, u & 0xffff0000u);
+    b -= __builtin_bit_cast(float, v & 0xffff0000u);
+    return __builtin_amdgcn_perm(v, u, 0x07060302u);
+}
+
 template <bool NT> __device__ __forceinline__ void dma16(uint64_t base, int off, uint32_t lds)
 {
     if constexpr (NT) dma16_to_lds_at_nt(base, off, lds);
     else dma16_to_lds_at(base, off, lds);
 }
 
-// R: tiles of a wave and round.  PIECES: the columns' copies take a weight's upper and lower bits; without, two MFMAs do
-template <int D, bool FAR, int NW, int R, bool PIECES>
+// R: tiles of a wave and round.  PIECES: how many of the three parts of a weight the copies of a head's column take
+template <int D, bool FAR, int NW, int R, int PIECES>
 __global__ void __launch_bounds__(64 * NW, 2)
 decode_kv4_kernel(const Args a)
 {
@@ -197,7 +212,7 @@ decode_kv4_kernel(const Args a)
     // this lane's column: head l16 % 2^lg, copy l16 / 2^lg
     const int hc = l16 & ((1 << a.lg) - 1), copy = l16 >> a.lg;
     const int mytile = R == 1 ? 0 : copy & (R - 1);
-    const bool lower = PIECES && (copy / R & 1);
+    const int piece = copy / R;
     const bool first = copy < R && hc < live;          // one column for each tile and head
     const long head = hq0 + min(hc, live - 1);
     const float c2 = SB_LOG2E / sqrtf((float)D);
@@ -337,16 +352,18 @@ decode_kv4_kernel(const Args a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] *= norm;
         // ---- output
-        // the upper half of a weight's bits is a bf16, what it leaves another one, rounded (16 bits in all; with PIECES each in its own columns)
-        u32x4 w0, w1;
+        // a weight is the sum of three bf16, of eight bits each: nothing of it is lost
+        u32x4 w0, w1, w2;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float a0 = w[2 * i], a1 = w[2 * i + 1];
-            const uint32_t u0 = __builtin_bit_cast(uint32_t, a0), u1 = __builtin_bit_cast(uint32_t, a1);
-            w0[i] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
-            const bf16x2 rest = {(__bf16)(a0 - __builtin_bit_cast(float, u0 & 0xffff0000u)), (__bf16)(a1 - __builtin_bit_cast(float, u1 & 0xffff0000u))};
-            w1[i] = __builtin_bit_cast(uint32_t, rest);
-            if (PIECES) w0[i] = lower ? w1[i] : w0[i];
+            float a0 = w[2 * i], a1 = w[2 * i + 1];
+            w0[i] = upper_halves(a0, a1);
+            w1[i] = upper_halves(a0, a1);
+            w2[i] = upper_halves(a0, a1);
+            if (PIECES > 1) w0[i] = piece == 0 ? w0[i] : w1[i];
+            if (PIECES > 2) w0[i] = piece < 2 ? w0[i] : w2[i];
+            // two tiles a wave, two copies for each: the third part goes to where the other tile's first one would be
+            if (PIECES == 2) w2[i] = piece == 0 ? R == 2 ? dpp_word<0x124>(w2[i]) : w2[i] : 0u;        // row_ror:4, to a copy of the other tile
         }
         if (more) dma_wait<P::LOADS>();    // V has landed
         else dma_wait<0>();
@@ -356,7 +373,7 @@ decode_kv4_kernel(const Args a)
             u32x4 wb = w0;
             if (R > 1) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) wb[i] = mytile == j ? wb[i] : 0u;
+                for (int i = 0; i < 4; ++i) wb[i] = mytile == j ? wb[i] : PIECES == 2 ? w2[i] : 0u;
             }
             // scales of the eight rows, bytes as they lie: of row i, the byte of this lane's columns to the exponent's place (what stands beside it does not count)
             constexpr int PER = 128 / D;   // rows in a word
@@ -389,7 +406,8 @@ decode_kv4_kernel(const Args a)
                 for (int i = 0; i < 4; ++i)
                     y[i] = __builtin_amdgcn_perm(pv[2 * i + 1][e >> 1], pv[2 * i][e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
                 const bf16x8 av = __builtin_bit_cast(bf16x8, y);
-                if (!PIECES) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, w1), acc[e], 0, 0, 0);
+                if (R * PIECES < 3) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, w2), acc[e], 0, 0, 0);
+                if (PIECES == 1) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, w1), acc[e], 0, 0, 0);
                 acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, __builtin_bit_cast(bf16x8, wb), acc[e], 0, 0, 0);
             }
         }
@@ -468,7 +486,7 @@ decode_kv4_kernel(const Args a)
         if (lq == 0) s_log[wave][l16] = lowhalf + upphalf;
     }
     barrier_lds();
-    constexpr int COPIES = R * (PIECES ? 2 : 1);           // columns of a head
+    constexpr int COPIES = R * PIECES;                     // columns of a head
     for (int i = tid; i < live * CH; i += NTHR) {
         const int g = i / CH, c = i % CH;
         f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -624,17 +642,23 @@ hipError_t launch_d(Args a, int B, int H, float* workspace, hipStream_t stream)
     hipError_t e = hipSuccess;
     while (1 << a.lg < std::min(a.G, GMAX)) ++a.lg;
     if (a.near > 0) {
-        const dim3 grid(bkv, 1u, nz), threads(64 * NEAR_NW);
-        if (a.lg == 4) hipLaunchKernelGGL((decode_kv4_kernel<D, false, NEAR_NW, 1, false>), grid, threads, 0, stream, a);
-        else if (a.lg < 3 && (long)bkv * nz > round_of(D)) hipLaunchKernelGGL((decode_kv4_kernel<D, false, NEAR_NW / 2, 2, true>), grid, dim3(32 * NEAR_NW), 0, stream, a);
-        else hipLaunchKernelGGL((decode_kv4_kernel<D, false, NEAR_NW, 1, true>), grid, threads, 0, stream, a);
+        const dim3 grid(bkv, 1u, nz);
+        const bool wide = a.lg < 3 && (long)bkv * nz > round_of(D);
+        auto go = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, stream, a); };
+        if (a.lg == 4) go(decode_kv4_kernel<D, false, NEAR_NW, 1, 1>, NEAR_NW);
+        else if (a.lg == 3) go(decode_kv4_kernel<D, false, NEAR_NW, 1, 2>, NEAR_NW);
+        else if (!wide) go(decode_kv4_kernel<D, false, NEAR_NW, 1, 3>, NEAR_NW);
+        else if (a.lg == 2) go(decode_kv4_kernel<D, false, NEAR_NW / 2, 2, 2>, NEAR_NW / 2);
+        else go(decode_kv4_kernel<D, false, NEAR_NW / 2, 2, 3>, NEAR_NW / 2);
         if ((e = hipGetLastError()) != hipSuccess || !combine) return e;
     }
     if (a.slots > (a.near > 0)) {
-        const dim3 grid((unsigned)(a.slots - (a.near > 0)), bkv, nz), threads(64 * FAR_NW);
-        if (a.lg == 4) hipLaunchKernelGGL((decode_kv4_kernel<D, true, FAR_NW, 1, false>), grid, threads, 0, stream, a);
-        else if (a.lg == 3) hipLaunchKernelGGL((decode_kv4_kernel<D, true, FAR_NW, 1, true>), grid, threads, 0, stream, a);
-        else hipLaunchKernelGGL((decode_kv4_kernel<D, true, FAR_NW, 2, true>), grid, threads, 0, stream, a);
+        const dim3 grid((unsigned)(a.slots - (a.near > 0)), bkv, nz);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * FAR_NW), 0, stream, a); };
+        if (a.lg == 4) go(decode_kv4_kernel<D, true, FAR_NW, 1, 1>);
+        else if (a.lg == 3) go(decode_kv4_kernel<D, true, FAR_NW, 1, 2>);
+        else if (a.lg == 2) go(decode_kv4_kernel<D, true, FAR_NW, 2, 2>);
+        else go(decode_kv4_kernel<D, true, FAR_NW, 2, 3>);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     const unsigned more = a.score_out ? bkv * (unsigned)a.slots : 0u;
