@@ -6,7 +6,7 @@
 // took (Eq. 2).
 //   near launch      grid (kv head, block of query heads): the nearest keys, all of a short cache
 //   far launch       grid (chunk, kv head, block of query heads): the keys before those; returns at once where the nearest keys
-//                    have used up the stick (CARRY_EXHAUSTED: every farther weight is zero in fp32)
+//                    have used up the stick (LEAST, below)
 //   combine launch   a workgroup per query head adds the chunks up in a fixed order; with scores, one per (kv head, chunk)
 //                    shifts the weights of its keys, sums them over the group's heads and adds the score
 //
@@ -16,8 +16,10 @@
 //            the same one), and converts them in registers, the scale with them.  Rows go to the MFMAs so that a lane gets eight
 //            consecutive keys of a head.
 //   weights  where the MFMA leaves the logits: Eq. 1's product over the lane's eight keys, then across the four lanes of a tile,
-//            the tiles and the waves (by LDS, one barrier a round).  What is left of the stick is carried as it is, not by its
-//            logarithm: the keys' scores are results in fp32.  From less than 2^-126 of it on, weights are subnormal at most and count as zero.
+//            the tiles and the waves (by LDS, one barrier a round).  The keys' scores are results in fp32, so what is left of the stick is carried as it is, not by its
+//            logarithm.  Many small weights would be lost where it is near 1: there their own sum P = prod (1 + e) - 1, e = sigma / (1 - sigma), is what is carried, up to a round of keys,
+//            and the rounds' shares of the stick are multiplied in 64 bits, as T / 256 factors that are alike round the same way (in fp32 throughout, T = 524288 and logits around
+//            -16: 3 % of the far weights, all of m).  That takes 2 to 8 % (B32 H16 T1800 d64, all far, 20.3 -> 21.9 us, d128 29.5 -> 29.8, B8 H16 T16384 d64 37.7 -> 39.5).  From less than 2^-126 of the stick on, weights are subnormal at most and count as zero.
 //   output   O^T[c][head] += V^T w: a lane's eight weights are the B operand as they lie; it loads D / 16 columns of those same
 //            eight rows of V, converts, and an in-register transposition (one v_perm per packed pair) makes the A operands.
 // Codes and scales come through LDS as whole rows, every wave its own, one round ahead: K's place is asked for again as soon as a round
@@ -52,7 +54,9 @@ struct Args {
     float* score_out;                  // nullptr: not wanted
     uint16_t* o;
     float* m;
-    float *part_o, *part_a, *part_l;   // [heads][slots][D], [heads][slots]: slot 0 the nearest; share of the stick that it leaves, and -log2 of that where m is wanted
+    float* part_o;                     // [heads][slots][D]: slot 0 the nearest
+    double* part_a;                    // [heads][slots]: share of the stick that a slot leaves
+    float* part_l;                     // and -log2 of it, where m is wanted
     float* wl;                         // [heads][Tcap]: weights inside their chunk, where scores are combined
     int T, Tcap, Hkv, G, near, C, slots;
     int lg;                            // log2 of the columns that a copy of the heads takes
@@ -99,11 +103,14 @@ __device__ __forceinline__ float wave_sum(float x)
 }
 
 // product over the lanes below this one, and over all in `total`
-template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_or_one(float x)
+template <int CTRL, int ROWS> __device__ __forceinline__ double dpp_or_one(double x)
 {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0x3f800000, __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false));
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0x3ff00000, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xF, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
-__device__ __forceinline__ float wave_prefix(float v, float& total)
+__device__ __forceinline__ double wave_prefix(double v, double& total)
 {
     v *= dpp_or_one<0x111, 0xF>(v);                       // row_shr:1, 2, 4, 8
     v *= dpp_or_one<0x112, 0xF>(v);
@@ -111,8 +118,21 @@ __device__ __forceinline__ float wave_prefix(float v, float& total)
     v *= dpp_or_one<0x118, 0xF>(v);
     v *= dpp_or_one<0x142, 0xA>(v);                       // row_bcast:15 into rows 1 and 3
     v *= dpp_or_one<0x143, 0xC>(v);                       // row_bcast:31 into rows 2 and 3
-    total = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 63);
+    total = __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
     return dpp_or_one<0x138, 0xF>(v);                     // wave_shr:1
+}
+
+// (1 + p) (1 + q) - 1
+__device__ __forceinline__ float plus(float p, float q) { return __builtin_fmaf(p, q, p + q); }
+
+// log2(1 + p), to some roundings of itself; below 1 / 4 by 2 atanh(p / (2 + p)), whose next term is 3e-9 of it
+__device__ __forceinline__ float log2_1p(float p)
+{
+    const float s = p * __builtin_amdgcn_rcpf(2.0f + p), y = s * s;
+    const float near_one = 2.0f * SB_LOG2E * (s + s * y * (1.0f / 3.0f + y * (1.0f / 5.0f + y * (1.0f / 7.0f))));
+    return p < 0.25f ? near_one : fast_log2(1.0f + p);
 }
 
 // `even`: v of this lane's column in row 0 (lanes 0 .. 31) or 2 (32 .. 63), `odd`: in row 1 or 3
@@ -190,7 +210,9 @@ decode_kv4_kernel(const Args a)
     constexpr int CW = D / 16;             // columns of V per lane
     constexpr int CH = D / 4;              // 16-byte chunks of a head's columns
     __shared__ __attribute__((aligned(16))) float tot[2][GMAX][NT];      // per round parity: what a tile leaves of the stick
+    __shared__ __attribute__((aligned(16))) float sums[2][GMAX][NT];     // and P of its keys
     __shared__ float s_log[NW][GMAX];
+    __shared__ double s_left[GMAX];
     using P = Place<D, R>;
     constexpr int SHARES = NW * GMAX * CH * 16;
     __shared__ __attribute__((aligned(1024))) char smem[NW * P::BYTES > SHARES ? NW * P::BYTES : SHARES];
@@ -229,7 +251,7 @@ decode_kv4_kernel(const Args a)
     f32x4 acc[CW];                         // O^T: row 4 lq + r of MFMA e is column CW (4 lq + r) + e, column l16
 #pragma unroll
     for (int e = 0; e < CW; ++e) acc[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    float stick = 1.0f, logs = 0.0f;       // left by the keys already passed; -log2 of what this lane's own keys left
+    double stick = 1.0, logs = 0.0;        // left by the keys already passed; -log2 of what this lane's own keys left
     int par = 0, hi = top;
 
     // ---- rows to LDS, whole rows of the wave's R tiles at a time; where a tile is below lo there is none, and the last one is loaded
@@ -306,51 +328,67 @@ decode_kv4_kernel(const Args a)
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the rows have been read)
         if (more) fetch_k(hi - KEYS);
-        // ---- the lane's chain: w[i] = e_i prod_{i' < i} (1 + e_i'), e = sigma / (1 - sigma); norm makes it the weight where the stick is whole
+        // ---- the lane's chain: w[i] = e_i prod_{i' < i} (1 + e_i'), their sum P; norm makes it the weight where the stick is whole
         // before the lane's nearest key, `leave` is what the eight keys leave
-        float w[8], norm, leave;
-        float W = 1.0f;
+        float w[8], norm, leave, P = 0.0f, run = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             x[i] *= c2;
-            w[i] = W * fast_exp2(x[i]);
-            W += w[i];
+            const float e = fast_exp2(x[i]);
+            w[i] = __builtin_fmaf(P, e, e);
+            P = __builtin_fmaf(P, 1.0f + e, e);            // (P + w would make the chain twice as long)
         }
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(W < 0x1p120f)) == 0, 1)) {
-            norm = leave = __builtin_amdgcn_rcpf(W);
-            if (a.m) logs += fast_log2(W);
-        } else {                           // in the log form
-            float run = 0.0f;
+        norm = leave = __builtin_amdgcn_rcpf(1.0f + P);
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(P < 0x1p40f)) != 0, 0)) {
+            // (norm times what is left before the lane could be subnormal where the weight is not)
 #pragma unroll
-            for (int i = 7; i >= 0; --i) {
-                run += sp2(x[i]);
-                w[i] = fast_exp2(x[i] - run);
-            }
+            for (int i = 0; i < 8; ++i) w[i] *= norm;
             norm = 1.0f;
-            leave = fast_exp2(-run);
-            logs += run;
+            if (!(P < 0x1p120f)) {         // in the log form
+#pragma unroll
+                for (int i = 7; i >= 0; --i) {
+                    run += sp2(x[i]);
+                    w[i] = fast_exp2(x[i] - run);
+                }
+                leave = fast_exp2(-run);
+            }
         }
+        if (a.m) logs += P < 0x1p120f ? log2_1p(P) : run;
         // ---- across the four lanes of a tile (the odd one of a pair and the upper half are nearer), the tiles and waves
         float even, odd, lowhalf, upphalf;
+        both_rows(P, even, odd);
+        both_halves(plus(even, odd), lowhalf, upphalf);
+        P = plus(lowhalf, upphalf);
         both_rows(leave, even, odd);
         both_halves(even * odd, lowhalf, upphalf);
         norm *= ((lq & 1) ? 1.0f : odd) * (lq < 2 ? upphalf : 1.0f);
-        if (lq == 0 && first) tot[par][hc][wave * R + mytile] = lowhalf * upphalf;
-        barrier_lds();
-        float before = stick;
         const int mine = wave * R + mytile;
+        if (lq == 0 && first) {
+            tot[par][hc][mine] = lowhalf * upphalf;
+            sums[par][hc][mine] = P;
+        }
+        barrier_lds();
+        const int row = min(hc, live - 1);
+        float before = (float)stick, left = 1.0f;
 #pragma unroll
         for (int j = 0; j < NT; j += 4) {
-            const f32x4 p = *reinterpret_cast<const f32x4*>(&tot[par][min(hc, live - 1)][j]);
+            const f32x4 p = *reinterpret_cast<const f32x4*>(&tot[par][row][j]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                before *= j + i < mine ? p[i] : 1.0f;
-                stick *= p[i];
+                if (j + i == mine) before *= left;
+                left *= p[i];
             }
         }
         norm *= before;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] *= norm;
+        // the round's P (a quarter of the tiles for each of a column's lanes); where the round takes half of the stick or more its last bits count no more, and it may be anything
+        P = sums[par][row][NT / 4 * lq];
+        if (NT == 8) P = plus(P, sums[par][row][2 * lq + 1]);
+        both_rows(P, even, odd);
+        both_halves(plus(even, odd), lowhalf, upphalf);
+        P = plus(lowhalf, upphalf);
+        stick *= left > 0.5f ? 1.0 - (double)(P * left) : (double)left;
         // ---- output
         // a weight is the sum of three bf16, of eight bits each: nothing of it is lost
         u32x4 w0, w1, w2;
@@ -478,10 +516,10 @@ decode_kv4_kernel(const Args a)
             r[(CW * lq + j) ^ (l16 & 7)] = y;
         }
     }
-    if (wave == 0 && lq == 0 && first && mytile == 0) tot[par][hc][0] = stick;
+    if (wave == 0 && lq == 0 && first && mytile == 0) s_left[hc] = stick;
     if (a.m) {
         float even, odd, lowhalf, upphalf;
-        both_rows(logs, even, odd);
+        both_rows((float)logs, even, odd);
         both_halves(even + odd, lowhalf, upphalf);
         if (lq == 0) s_log[wave][l16] = lowhalf + upphalf;
     }
@@ -497,7 +535,7 @@ decode_kv4_kernel(const Args a)
                 const int col = g + (k << a.lg);
                 s += ored[(w * GMAX + col) * CH + (c ^ (col & 7))];
             }
-        const float left = tot[par][g][0];
+        const double left = s_left[g];
         float log = 0.0f;
         if (a.m && c == 0)
             for (int w = 0; w < NW; ++w)
@@ -508,7 +546,7 @@ decode_kv4_kernel(const Args a)
             if (a.rb) {
                 const uint16_t* e = a.rb + ((bkv % a.Hkv) * (long)a.G + g0 + g) * D + 4 * c;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) s[k] += left * __builtin_bit_cast(float, (uint32_t)e[k] << 16);
+                for (int k = 0; k < 4; ++k) s[k] += (float)left * __builtin_bit_cast(float, (uint32_t)e[k] << 16);
             }
             *reinterpret_cast<bf16x4*>(a.o + h * D + 4 * c) = bf16x4{(__bf16)s[0], (__bf16)s[1], (__bf16)s[2], (__bf16)s[3]};
             if (a.m && c == 0) a.m[h] = -log * SB_LN2;
@@ -541,7 +579,7 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
     if ((int)blockIdx.x < heads) {
         const long bh = blockIdx.x;
         const int n = slots_of(a, up32(length_of(a, (int)(bh / H))));
-        const float* pa = a.part_a + bh * a.slots;
+        const double* pa = a.part_a + bh * a.slots;
         if (!a.m && a.near > 0 && pa[0] < LEAST) return;               // finished by the near launch
         if (a.slots == 1) return;                                      // (so is every head)
         // slot i gets what the nearer (lower) slots left
@@ -552,14 +590,14 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
         f32x4 x[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = grp + i * NG < n ? po[(grp + i * NG) * NV] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        float p[2];
+        double p[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) p[e] = 2 * lane + e < n ? pa[2 * lane + e] : 1.0f;
-        float left;
-        const float before = wave_prefix(p[0] * p[1], left);
+        for (int e = 0; e < 2; ++e) p[e] = 2 * lane + e < n ? pa[2 * lane + e] : 1.0;
+        double left;
+        const double before = wave_prefix(p[0] * p[1], left);
         if (wave == 0) {
-            f[2 * lane] = before;
-            f[2 * lane + 1] = before * p[0];
+            f[2 * lane] = (float)before;
+            f[2 * lane + 1] = (float)(before * p[0]);
         }
         __syncthreads();
         f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -571,7 +609,7 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
             float r = 0.0f;
 #pragma unroll
             for (int g = 0; g < NG; ++g) r += ored[g][tid];
-            if (a.rb) r += left * __builtin_bit_cast(float, (uint32_t)a.rb[(bh % H) * D + tid] << 16);
+            if (a.rb) r += (float)left * __builtin_bit_cast(float, (uint32_t)a.rb[(bh % H) * D + tid] << 16);
             const __bf16 val = (__bf16)r;
             a.o[bh * D + tid] = __builtin_bit_cast(uint16_t, val);
         }
@@ -594,17 +632,17 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
     const long hq0 = (long)bkv * a.G;
     bool any = false;
     for (int g = wave; g < a.G; g += COMBINE_THREADS / 64) {
-        const float* pa = a.part_a + (hq0 + g) * a.slots;
-        float x = 1.0f;
-        for (int i = lane; i < slot; i += 64) x *= pa[i];
-        wave_prefix(x, x);
+        const double* pa = a.part_a + (hq0 + g) * a.slots;
+        double before = 1.0;
+        for (int i = lane; i < slot; i += 64) before *= pa[i];
+        wave_prefix(before, before);
         // the far launch left out the blocks of heads that are all exhausted
         bool there = true;
         if (!a.m && a.near > 0 && slot > 0) {
             const int g0 = g / GMAX * GMAX;
             there = __builtin_amdgcn_ballot_w64(!(a.part_a[(hq0 + min(g0 + (lane & 15), min(a.G, g0 + GMAX) - 1)) * a.slots] < LEAST)) != 0;
         }
-        x = there ? x : 0.0f;
+        const float x = there ? (float)before : 0.0f;
         any |= x != 0.0f;
         if (lane == 0) f[g] = x;
     }
@@ -635,9 +673,9 @@ hipError_t launch_d(Args a, int B, int H, float* workspace, hipStream_t stream)
     const bool combine = a.slots > 1 || (a.score_out && a.G > GMAX);
     if (combine) {
         a.part_o = workspace;
-        a.part_a = a.part_o + heads * a.slots * D;
-        a.part_l = a.part_a + heads * a.slots;
-        if (a.score_out) a.wl = a.part_a + ((2 * heads * a.slots + 3) & ~3L);
+        a.part_a = reinterpret_cast<double*>(a.part_o + heads * a.slots * D);
+        a.part_l = reinterpret_cast<float*>(a.part_a + heads * a.slots);
+        if (a.score_out) a.wl = a.part_o + heads * a.slots * D + ((3 * heads * a.slots + 3) & ~3L);
     }
     hipError_t e = hipSuccess;
     while (1 << a.lg < std::min(a.G, GMAX)) ++a.lg;
@@ -675,7 +713,7 @@ size_t decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d,
 {
     const long heads = (long)B * H;
     const long slots = std::max(split_for(B, H, Hkv, T, d, false).slots, split_for(B, H, Hkv, T, d, true).slots);
-    size_t n = (size_t)heads * slots * d + (size_t)((2 * heads * slots + 3) & ~3L);
+    size_t n = (size_t)heads * slots * d + (size_t)((3 * heads * slots + 3) & ~3L);
     if (scores) n += (size_t)heads * Tcap;
     return sizeof(float) * n;
 }
