@@ -3,7 +3,8 @@
 //
 // Logits as in the forward, S^T = K Q^T by the 32x32x16 MFMA, a lane 16 keys of one query; Eq. 1's product along the keys in the lane,
 // and what is left of a query's stick carried from 32 keys to the next as it is, not by its logarithm: a weight here is a result in
-// fp32, and the logarithm of a carry around 30 would be off by 2^-20 of it (the forward's weights go on to a product in bf16).  From
+// fp32, and the logarithm of a carry around 30 would be off by 2^-20 of it (the forward's weights go on to a product in bf16).  As in sb_decode_kv4.hip, many small weights would be
+// lost beside a 1: the keys of a tile carry P = prod (1 + e) - 1, and the tiles' shares of the stick are multiplied in 64 bits.  From
 // less than 2^-126 of the stick on, no weight is more than a subnormal number: the row counts as exhausted and what is farther gets nothing from it.
 // In place of A V the sum of A over the queries.  A unit is 32 query rows of one head; units of the heads of a group at the
 // same rows are neighbours, as they read the same keys.  What a workgroup's queries give the keys, one number a key, goes into
@@ -13,8 +14,8 @@
 //                            second one the weights
 //   key_weight_small_kernel  one unit a workgroup, its waves 32 keys each, side by side
 // Bound by vector instructions: for 32 x 32 weights 16 exponentials a lane and some 110 others, next to the D / 16 matrix products.  B1 H32 Hkv8 T8192 d128,
-// 1.05 million such squares, all far 401 us, a third of the kv heads 188, none 40; the products alone are 216 us at the 1271 TFLOP/s that a product of 8192^3 reaches
-// here (109 at the chip's peak), the exponentials alone 109 at 2.4 GHz.  Three and four tiles of K under way instead of two, or four waves a unit, gain nothing (402 -> 482 with four).
+// 1.05 million such squares, all far 405 us, a third of the kv heads 186, none 40 (384 all far with 1 + P and fp32 in place of P and 64 bits); the products alone are 216 us at the 1271 TFLOP/s that a product of 8192^3 reaches
+// here (109 at the chip's peak), the exponentials alone 109 at 2.4 GHz.  Three and four tiles of K under way instead of two, or four waves a unit, gain nothing (402 -> 482 with four, before that).
 #include <climits>
 #include <type_traits>
 #include "sb_kernels.h"
@@ -62,7 +63,7 @@ struct Args {
     float* score_out;
     float* part;                       // [entry * kv head][group][Tpad]; a group is a workgroup's units
     int* reach;                        // [entry * kv head][group][chunks][2]: first key written, one past the last
-    float* left;                       // [entry * kv head][unit][chunks][32]: the share of the stick that a chunk leaves of each query's
+    double* left;                      // [entry * kv head][unit][chunks][32]: the share of the stick that a chunk leaves of each query's
     int H, Hkv, G, Tq, T, Tcap, Tpad, groups, chunks, C;
 };
 
@@ -72,56 +73,78 @@ __device__ __forceinline__ int length_of(const int* lens, int b, int most)
 }
 
 constexpr float LEAST = 0x1p-126f;     // of the stick
-__device__ __forceinline__ bool none_left(float stick) { return __builtin_amdgcn_ballot_w64(!(stick < LEAST)) == 0; }
+__device__ __forceinline__ bool none_left(double stick) { return __builtin_amdgcn_ballot_w64(!(stick < LEAST)) == 0; }
 
 // One query's share of 32 keys, a half-wave 16 of them, N times (two subtiles of keys, or two queries): with the stick whole before a subtile's nearest
-// key, the weight of key r is w[r] * mine, and `all` is what its 32 leave.  MASK: keys from `visible` on are not seen.  (N = 2: one's instructions fill the
+// key, the weight of key r is w[r] * mine, and `all` is what its 32 leave, 1 / (1 + sum).  MASK: keys from `visible` on are not seen.  (N = 2: one's instructions fill the
 // other's waits.)
-template <int N> using f32xn = float __attribute__((ext_vector_type(N)));
-template <bool MASK, int N>
-__device__ __forceinline__ void weights(const f32x16 (&s)[N], float c2, const int (&visible)[N], int hh, float (&w)[N][16], f32xn<N>& mine, f32xn<N>& all)
+struct Taken { float all, sum; };
+// (1 + p) (1 + q) - 1
+__device__ __forceinline__ float plus(float p, float q) { return __builtin_fmaf(p, q, p + q); }
+// of one's keys and the next, farther ones'
+__device__ __forceinline__ Taken both(Taken x, Taken y) { return {x.all * y.all, plus(x.sum, y.sum)}; }
+// What is left once these keys have been passed.  Where they take half of the stick or more, the last bits of the sum count no more, and it may be anything.
+__device__ __forceinline__ double passed(double stick, Taken t)
 {
-    // w[r] = W_r e_r, W_{r+1} = W_r + w[r], e = sigma / (1 - sigma): W_r = prod_{r' < r} 1 / (1 - sigma_r')
-    float W[N], most = 0.0f;
+    return stick * (t.all > 0.5f ? 1.0 - (double)(t.all * t.sum) : (double)t.all);
+}
+template <bool MASK, int N>
+__device__ __forceinline__ void weights(const f32x16 (&s)[N], float c2, const int (&visible)[N], int hh, float (&w)[N][16], float (&mine)[N], Taken (&t)[N])
+{
+    // w[r] = (1 + P_r) e_r, P_{r+1} = P_r + w[r], e = sigma / (1 - sigma): 1 + P_r = prod_{r' < r} 1 / (1 - sigma_r')
+    float P[N], most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) W[i] = 1.0f;
+    for (int i = 0; i < N; ++i) P[i] = 0.0f;
 #pragma unroll
     for (int r = 0; r < 16; ++r)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float e = fast_exp2(s[i][r] * c2);
             if (MASK) e = r < visible[i] ? e : 0.0f;
-            w[i][r] = W[i] * e;
-            W[i] += w[i][r];
+            w[i][r] = __builtin_fmaf(P[i], e, e);
+            P[i] += w[i][r];
         }
 #pragma unroll
-    for (int i = 0; i < N; ++i) most += W[i];
+    for (int i = 0; i < N; ++i) most += P[i];
     // what the lane's keys leave, and what makes w the weight where the stick is whole before the lane's nearest key
     float left[N], norm[N];
-    const bool logs = __builtin_amdgcn_ballot_w64(!(most < 0x1p120f)) != 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) left[i] = norm[i] = __builtin_amdgcn_rcpf(W[i]);
-    if (__builtin_expect(logs, 0)) {
+    for (int i = 0; i < N; ++i) left[i] = norm[i] = __builtin_amdgcn_rcpf(1.0f + P[i]);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(most < 0x1p40f)) != 0, 0)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float run = 0.0f;
+            // (norm times what is left before the lane could be subnormal where the weight is not)
 #pragma unroll
-            for (int r = 15; r >= 0; --r) {
-                const float x = !MASK || r < visible[i] ? s[i][r] * c2 : -INFINITY;
-                run += sp2(x);
-                w[i][r] = fast_exp2(x - run);
-            }
-            left[i] = fast_exp2(-run);
+            for (int r = 0; r < 16; ++r) w[i][r] *= norm[i];
             norm[i] = 1.0f;
+            if (!(P[i] < 0x1p120f)) {          // in the log form
+                float run = 0.0f;
+#pragma unroll
+                for (int r = 15; r >= 0; --r) {
+                    const float x = !MASK || r < visible[i] ? s[i][r] * c2 : -INFINITY;
+                    run += sp2(x);
+                    w[i][r] = fast_exp2(x - run);
+                }
+                left[i] = fast_exp2(-run);
+            }
         }
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        float lo, hi;                          // (the upper half's keys are nearer)
+        float lo, hi, p, q;                    // (the upper half's keys are nearer)
         both_halves(left[i], lo, hi);
-        all[i] = lo * hi;
+        both_halves(P[i], p, q);
+        t[i] = {lo * hi, plus(p, q)};
         mine[i] = hh ? norm[i] : norm[i] * hi;
     }
+}
+
+// the other half-wave's copy
+__device__ __forceinline__ double other_half(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)u, 32), hi = (uint32_t)__shfl_xor((int)(uint32_t)(u >> 32), 32);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
 // the unit's rows and what they see
@@ -222,14 +245,14 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     const int off = len - qlen;                                         // position of query row 0
     const int unit = (grp * NW + wave) * NU;
     int* const reach = a.reach + (((long)bkv * a.groups + grp) * a.chunks + chunk) * 2;
-    float* const left = a.left + (((long)bkv * a.groups * NW + unit) * a.chunks) * 32 + n;       // of chunk 0
+    double* const left = a.left + (((long)bkv * a.groups * NW + unit) * a.chunks) * 32 + n;       // of chunk 0
     Unit u[NU];
-    f32xn<NU> stick;
+    double stick[NU];
     int all_see = INT_MAX, some_see = 0;                                // (as Unit's)
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
         u[i] = unit_of(a, unit + i, bkv, off, qlen, n);
-        stick[i] = u[i].there ? 1.0f : 0.0f;
+        stick[i] = u[i].there ? 1.0 : 0.0;
         all_see = min(all_see, u[i].all);
         some_see = max(some_see, u[i].some);
     }
@@ -253,17 +276,15 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     if constexpr (WHAT == 2) {
         // what the nearer chunks left: every second one a half-wave's, eight loads at once
         constexpr int EACH = 8;
-        float mine = 1.0f;
+        double mine = 1.0;
         for (int c = a.chunks - 1 - hh; c > chunk; c -= 2 * EACH) {
-            float x[EACH];
+            double x[EACH];
 #pragma unroll
             for (int i = 0; i < EACH; ++i) x[i] = left[max(c - 2 * i, chunk + 1) * 32];
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) mine *= c - 2 * i > chunk ? x[i] : 1.0f;
+            for (int i = 0; i < EACH; ++i) mine *= c - 2 * i > chunk ? x[i] : 1.0;
         }
-        float lo_half, hi_half;
-        both_halves(mine, lo_half, hi_half);
-        stick[0] *= lo_half * hi_half;
+        stick[0] *= mine * other_half(mine);
         const int done = none_left(stick[0]) ? -1 : 0;
         if (lane == 0) s_done[0][wave] = done;
         barrier_lds();
@@ -328,25 +349,30 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
             if ((NU == 1 ? base - 32 : base) >= some_see || none_left(left_of())) continue;
             f32x16 s[2];
             float w[2][16];
-            f32xn<2> mine, all;
+            float mine[2];
+            Taken t[2];
             logits<D, NU>(s, qf, aoff, par * TILE + (1 - half) * C::SUB);
             const int seen[2] = {u[0].sees - base - 16 * hh, (NU == 1 ? u[0].sees + 32 : u[NU - 1].sees) - base - 16 * hh};
-            if (base + 32 > all_see) weights<true>(s, c2, seen, hh, w, mine, all);
-            else weights<false>(s, c2, seen, hh, w, mine, all);
+            if (base + 32 > all_see) weights<true>(s, c2, seen, hh, w, mine, t);
+            else weights<false>(s, c2, seen, hh, w, mine, t);
             if constexpr (NU == 1) {
+                if constexpr (WHAT != 1) {
+                    mine[0] *= (float)stick[0];
+                    mine[1] *= (float)stick[0] * t[0].all;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if constexpr (WHAT != 1) {
-                        mine[i] *= stick[0];
+                    for (int i = 0; i < 2; ++i) {
 #pragma unroll
                         for (int r = 0; r < 16; ++r) w[i][r] *= mine[i];
                         sum[i] = sums_of_lanes(w[i], n);
                     }
-                    stick[0] *= all[i];
                 }
+                stick[0] = passed(stick[0], both(t[0], t[1]));
             } else {
-                mine *= stick;
-                stick *= all;
+#pragma unroll
+                for (int i = 0; i < NU; ++i) {
+                    mine[i] *= (float)stick[i];
+                    stick[i] = passed(stick[i], t[i]);
+                }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) w[0][r] = w[0][r] * mine[0] + w[1][r] * mine[1];
                 sum[half] = sums_of_lanes(w[0], n);
@@ -376,7 +402,7 @@ key_weight_small_kernel(const Args a)
     using C = Cfg<D>;
     __shared__ __attribute__((aligned(1024))) char rows[SNW * C::SUB];      // 32 of K a wave
     __shared__ __attribute__((aligned(1024))) char qrows[C::SUB];
-    __shared__ __attribute__((aligned(16))) float prod[2][SNW][32];         // per round parity: what a wave's keys leave
+    __shared__ __attribute__((aligned(16))) Taken prod[2][SNW][32];         // per round parity: a wave's keys
     const int unit = a.groups - 1 - (int)blockIdx.x, bkv = blockIdx.y;
     const int b = bkv / a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -385,7 +411,7 @@ key_weight_small_kernel(const Args a)
     const int len = length_of(a.lens, b, a.T), qlen = length_of(a.qlens, b, a.Tq);
     const Unit u = unit_of(a, unit, bkv, len - qlen, qlen, n);
     int* const reach = a.reach + ((long)bkv * a.groups + unit) * 2;
-    float stick = u.there ? 1.0f : 0.0f;
+    double stick = u.there ? 1.0 : 0.0;
     if (u.some == 0) {
         if (tid == 0) reach[0] = reach[1] = 0;
         return;
@@ -426,23 +452,25 @@ key_weight_small_kernel(const Args a)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (the rows have been read)
         if (hi > 32 * SNW) fetch(base - 32 * SNW);
         float w[1][16];
-        f32xn<1> mine = 0.0f, all = 1.0f;
+        float mine[1] = {0.0f};
+        Taken t[1] = {{1.0f, 0.0f}};
         if (base >= 0) {
-            if (base + 32 > u.all) weights<true>(s, c2, {u.sees - base - 16 * hh}, hh, w, mine, all);
-            else weights<false>(s, c2, {0}, hh, w, mine, all);
+            if (base + 32 > u.all) weights<true>(s, c2, {u.sees - base - 16 * hh}, hh, w, mine, t);
+            else weights<false>(s, c2, {0}, hh, w, mine, t);
         } else {
 #pragma unroll
             for (int r = 0; r < 16; ++r) w[0][r] = 0.0f;
         }
-        if (hh == 0) prod[par][wave][n] = all[0];
+        if (hh == 0) prod[par][wave][n] = t[0];
         barrier_lds();
-        float before = stick;
+        float before = (float)stick;
+        Taken round = {1.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < SNW; ++j) {
-            const float p = prod[par][j][n];
-            if (j < wave) before *= p;
-            stick *= p;
+            if (j == wave) before *= round.all;
+            round = both(round, prod[par][j][n]);
         }
+        stick = passed(stick, round);
         if (base >= 0) {
             mine[0] *= before;
 #pragma unroll
@@ -502,7 +530,7 @@ struct Plan {
     int groups, chunks, C;
     int Tpad;
     int units() const { return small ? groups : groups * NW; }
-    size_t floats(int BHkv) const { return (size_t)BHkv * ((size_t)groups * (Tpad + 2 * (size_t)chunks) + (chunks > 1 ? (size_t)units() * chunks * 32 : 0)); }
+    size_t floats(int BHkv) const { return (size_t)BHkv * ((size_t)groups * (Tpad + 2 * (size_t)chunks) + (chunks > 1 ? (size_t)units() * chunks * 64 : 0)); }
 };
 // What a plan takes, from measurements (all heads far; us).  One unit a workgroup: 1.25 for a round of 256 keys, of the longest unit alone where the
 // units fit the chip, 256 of them at a time beyond.  Four units: 1.4 for a tile of 64 keys of the longest, or 0.45 ns a subtile of all, whichever is more.  Chunks of
@@ -568,7 +596,7 @@ hipError_t launch_key_weight(const uint16_t* q, const uint16_t* k, const int* le
     const Plan p = plan_of(B, H, Hkv, Tq, T);
     const int BHkv = B * Hkv;
     Args a = {q, k, lens, qlens, score, score_out, workspace, nullptr, nullptr, H, Hkv, H / Hkv, Tq, T, Tcap, p.Tpad, p.groups, p.chunks, p.C};
-    a.left = workspace + (size_t)BHkv * p.groups * p.Tpad;
+    a.left = reinterpret_cast<double*>(workspace + (size_t)BHkv * p.groups * p.Tpad);
     a.reach = reinterpret_cast<int*>(a.left + (p.chunks > 1 ? (size_t)BHkv * p.units() * p.chunks * 32 : 0));
     const hipError_t e = d == 32 ? launch_d<32>(a, p, BHkv, stream) : d == 64 ? launch_d<64>(a, p, BHkv, stream) : launch_d<128>(a, p, BHkv, stream);
     if (e != hipSuccess) return e;
