@@ -269,7 +269,8 @@ int sb_attn_kv4_load(const void* kc, const void* ks, const void* vc, const void*
  * 1024 query heads a kv head and B*H <= 8388607 with score_out (16777215 without).
  * Weights have fp32's 24 bits, in o (which is rounded once, at its end) and in score.  Rows of
  * which less than 2^-126 of the stick is left count as zero, a NaN among them too, as long as m is not wanted.
- * workspace: sb_attn_decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, score_out != NULL) bytes.
+ * workspace: sb_attn_decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, score_out != NULL) bytes: 4*d + 12 a query head and
+ * chunk (at most 128), and with scores 4*T a query head where it has more than one chunk or a kv head more than 16.
  * Bit-reproducible, as sb_attn_decode.
  */
 size_t sb_attn_decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d, int scores);

@@ -369,7 +369,7 @@ int check_decode_kv4(int B, int H, int Hkv, int T, int Tcap, int d, bool scores)
 size_t sb_attn_decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d, int scores)
 {
     if (check_decode_kv4(B, H, Hkv, T, Tcap, d, scores != 0) != SB_OK) return 0;
-    return sb::decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, scores != 0);
+    return sb::decode_kv4_workspace_bytes(B, H, Hkv, T, d, scores != 0);
 }
 
 int sb_attn_decode_kv4(const void* q, const void* kc, const void* ks, const void* vc, const void* vs, const void* r, const int* lens,
@@ -382,7 +382,7 @@ int sb_attn_decode_kv4(const void* q, const void* kc, const void* ks, const void
         !aligned16(score) || !aligned16(score_out) || !aligned16(o) || !aligned16(m) || !aligned16(workspace))
         return SB_ERR_ALIGN;
     if (scores_overlap(score, score_out, B, Hkv, Tcap)) return SB_ERR_OVERLAP;
-    if (!workspace || workspace_bytes < sb::decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, score_out != nullptr)) return SB_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < sb::decode_kv4_workspace_bytes(B, H, Hkv, T, d, score_out != nullptr)) return SB_ERR_WORKSPACE;
     hipError_t e = sb::launch_decode_kv4(static_cast<const uint16_t*>(q), in_bytes(kc), in_bytes(ks), in_bytes(vc), in_bytes(vs), static_cast<const uint16_t*>(r),
                                          lens, score, score_out, static_cast<uint16_t*>(o), m, static_cast<float*>(workspace),
                                          B, H, Hkv, T, Tcap, d, static_cast<hipStream_t>(stream));

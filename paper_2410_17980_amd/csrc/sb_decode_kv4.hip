@@ -57,8 +57,8 @@ struct Args {
     float* part_o;                     // [heads][slots][D]: slot 0 the nearest
     double* part_a;                    // [heads][slots]: share of the stick that a slot leaves
     float* part_l;                     // and -log2 of it, where m is wanted
-    float* wl;                         // [heads][Tcap]: weights inside their chunk, where scores are combined
-    int T, Tcap, Hkv, G, near, C, slots;
+    float* wl;                         // [heads][rows]: weights inside their chunk, where scores are combined; T rows, in whole tiles
+    int T, rows, Tcap, Hkv, G, near, C, slots;
     int lg;                            // log2 of the columns that a copy of the heads takes
 };
 
@@ -454,7 +454,7 @@ decode_kv4_kernel(const Args a)
             if (a.wl) {
                 const int base = hi - KW * (mine + 1);
                 if (first && base >= lo) {
-                    float* p = a.wl + (hq0 + hc) * a.Tcap + base + 8 * lq;
+                    float* p = a.wl + (hq0 + hc) * a.rows + base + 8 * lq;
                     *reinterpret_cast<f32x4*>(p) = f32x4{w[0], w[1], w[2], w[3]};
                     *reinterpret_cast<f32x4*>(p + 4) = f32x4{w[4], w[5], w[6], w[7]};
                 }
@@ -503,7 +503,7 @@ decode_kv4_kernel(const Args a)
         for (int i = lo + tid; i < hi; i += NTHR) a.score_out[(long)bkv * a.Tcap + i] = a.score ? a.score[(long)bkv * a.Tcap + i] : 0.0f;
     if (!FAR && a.wl && a.slots == 1)                      // (read by the combination)
         for (int g = 0; g < live; ++g)
-            for (int i = lo + tid; i < hi; i += NTHR) a.wl[(hq0 + g) * a.Tcap + i] = 0.0f;
+            for (int i = lo + tid; i < hi; i += NTHR) a.wl[(hq0 + g) * a.rows + i] = 0.0f;
 
     // ---- the columns' and waves' shares: a lane holds 4 CW columns of V of its column, CW chunks of 16 bytes, their places xor-ed with the column
     {
@@ -651,7 +651,7 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
     for (int i = lo + 4 * tid; i < min(top, len); i += 4 * COMBINE_THREADS) {
         f32x4 s = a.score ? *reinterpret_cast<const f32x4*>(a.score + row + i) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         for (int g = 0; g < a.G; ++g)
-            if (f[g] != 0.0f) s += f[g] * *reinterpret_cast<const f32x4*>(a.wl + (hq0 + g) * a.Tcap + i);
+            if (f[g] != 0.0f) s += f[g] * *reinterpret_cast<const f32x4*>(a.wl + (hq0 + g) * a.rows + i);
         if (i + 4 <= len) {
             *reinterpret_cast<f32x4*>(a.score_out + row + i) = s;
         } else {
@@ -665,12 +665,15 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
 // Workgroups of the near launch that one round of the chip holds: eight waves of 146 registers and 68 KB, 112 and 35 KB, 89 and 19 KB.
 constexpr long round_of(int d) { return d == 128 ? 256 : 512; }
 
+// the heads' weights meet in a launch of their own
+inline bool combined(long slots, int G) { return slots > 1 || G > GMAX; }
+
 template <int D>
 hipError_t launch_d(Args a, int B, int H, float* workspace, hipStream_t stream)
 {
     const long heads = (long)B * H;
     const unsigned bkv = (unsigned)(B * a.Hkv), nz = (unsigned)((a.G + GMAX - 1) / GMAX);
-    const bool combine = a.slots > 1 || (a.score_out && a.G > GMAX);
+    const bool combine = a.slots > 1 || (a.score_out && combined(a.slots, a.G));
     if (combine) {
         a.part_o = workspace;
         a.part_a = reinterpret_cast<double*>(a.part_o + heads * a.slots * D);
@@ -709,12 +712,12 @@ hipError_t launch_d(Args a, int B, int H, float* workspace, hipStream_t stream)
 int decode_kv4_most_group() { return MOST_GROUP; }
 
 // room for either split
-size_t decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d, bool scores)
+size_t decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int d, bool scores)
 {
     const long heads = (long)B * H;
     const long slots = std::max(split_for(B, H, Hkv, T, d, false).slots, split_for(B, H, Hkv, T, d, true).slots);
     size_t n = (size_t)heads * slots * d + (size_t)((3 * heads * slots + 3) & ~3L);
-    if (scores) n += (size_t)heads * Tcap;
+    if (scores && combined(slots, H / Hkv)) n += (size_t)heads * ((T + KW - 1) / KW * KW);
     return sizeof(float) * n;
 }
 
@@ -723,7 +726,7 @@ hipError_t launch_decode_kv4(const uint16_t* q, const uint8_t* kc, const uint8_t
                              int B, int H, int Hkv, int T, int Tcap, int d, hipStream_t stream)
 {
     const Split s = split_for(B, H, Hkv, T, d, m != nullptr);
-    const Args a = {q, kc, ks, vc, vs, rb, lens, score, score_out, o, m, nullptr, nullptr, nullptr, nullptr, T, Tcap, Hkv, H / Hkv, s.near, s.C, s.slots, 0};
+    const Args a = {q, kc, ks, vc, vs, rb, lens, score, score_out, o, m, nullptr, nullptr, nullptr, nullptr, T, (T + KW - 1) / KW * KW, Tcap, Hkv, H / Hkv, s.near, s.C, s.slots, 0};
     if (d == 32) return launch_d<32>(a, B, H, workspace, stream);
     if (d == 64) return launch_d<64>(a, B, H, workspace, stream);
     return launch_d<128>(a, B, H, workspace, stream);

@@ -93,7 +93,7 @@ hipError_t launch_kv4_load(const uint8_t* kc, const uint8_t* ks, const uint8_t* 
 // Single-token decode on a 4-bit cache, Tcap a multiple of 32.  lens: rows per entry on the device, or nullptr: T.
 // score, score_out: [B][Hkv][Tcap] or nullptr; workspace: decode_kv4_workspace_bytes bytes.
 int decode_kv4_most_group();               // query heads of a kv head, with scores
-size_t decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int Tcap, int d, bool scores);
+size_t decode_kv4_workspace_bytes(int B, int H, int Hkv, int T, int d, bool scores);
 hipError_t launch_decode_kv4(const uint16_t* q, const uint8_t* kc, const uint8_t* ks, const uint8_t* vc, const uint8_t* vs, const uint16_t* rb,
                              const int* lens, const float* score, float* score_out, uint16_t* o, float* m, float* workspace,
                              int B, int H, int Hkv, int T, int Tcap, int d, hipStream_t stream);
