@@ -289,7 +289,8 @@ int sb_attn_decode_kv4(const void* q, const void* kc, const void* ks, const void
  * stands at row lens[b] - qlens[b] + t and weighs the keys before it.  Tq = T: the whole prompt;
  * Tq = 1, its key appended already: one token.  1 <= Tq <= T <= Tcap, T <= 524288, B*Hkv <= 65535.
  * workspace: sb_attn_key_weight_workspace_bytes(B, H, Hkv, Tq, T, d) bytes, at most about 4*T for each 128
- * query rows of a head (for each 32 where there are few).  Bit-reproducible.
+ * query rows of a head (for each 32 where there are few), and no more than 2 GiB or 4*T a kv head, whichever is more, and a few MB:
+ * longer prompts go through it part by part.  Bit-reproducible.
  */
 size_t sb_attn_key_weight_workspace_bytes(int B, int H, int Hkv, int Tq, int T, int d);
 int sb_attn_key_weight(const void* q, const void* k, const int* lens, const int* qlens, const float* score, float* score_out,

@@ -61,10 +61,10 @@ struct Args {
     const int *lens, *qlens;           // or nullptr: T, Tq
     const float* score;                // or nullptr: zero
     float* score_out;
-    float* part;                       // [entry * kv head][group][Tpad]; a group is a workgroup's units
+    float* part;                       // [entry * kv head][group][Tpad]; a group is a workgroup's units, groups first .. first + groups - 1
     int* reach;                        // [entry * kv head][group][chunks][2]: first key written, one past the last
     double* left;                      // [entry * kv head][unit][chunks][32]: the share of the stick that a chunk leaves of each query's
-    int H, Hkv, G, Tq, T, Tcap, Tpad, groups, chunks, C;
+    int H, Hkv, G, Tq, T, Tcap, Tpad, groups, chunks, C, first;
 };
 
 __device__ __forceinline__ int length_of(const int* lens, int b, int most)
@@ -235,7 +235,7 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
 
     // The longest first; kv heads turn as workgroups go round the chip, so that a CU does not get the same one, which may be the one that reaches far, each time
     const int wg = first_wg + blockIdx.x, chunk = WHAT ? blockIdx.y : 0;
-    const int turn = wg / BHkv, grp = a.groups - 1 - turn;
+    const int turn = wg / BHkv, at = a.groups - 1 - turn, grp = a.first + at;
     const int bkv = (wg % BHkv + (int)((long)turn * BHkv / 256 % BHkv)) % BHkv;
     const int b = bkv / a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -244,7 +244,7 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     const int len = length_of(a.lens, b, a.T), qlen = length_of(a.qlens, b, a.Tq);
     const int off = len - qlen;                                         // position of query row 0
     const int unit = (grp * NW + wave) * NU;
-    int* const reach = a.reach + (((long)bkv * a.groups + grp) * a.chunks + chunk) * 2;
+    int* const reach = a.reach + (((long)bkv * a.groups + at) * a.chunks + chunk) * 2;
     double* const left = a.left + (((long)bkv * a.groups * NW + unit) * a.chunks) * 32 + n;       // of chunk 0
     Unit u[NU];
     double stick[NU];
@@ -326,7 +326,7 @@ key_weight_kernel(const Args a, int BHkv, int first_wg)
     for (int s = 0; s < D / 16; ++s) aoff[s] = smem0 + tile_off_perm<D>(perm_row(n), 2 * s + hh);
 
     const int jt0 = (top - 1) / TK, jend = lo / TK;
-    float* const part = a.part + ((long)bkv * a.groups + grp) * a.Tpad;
+    float* const part = a.part + ((long)bkv * a.groups + at) * a.Tpad;
     auto flush = [&](int jt, int par) __attribute__((always_inline)) {
         if (tid < TK) part[(long)jt * TK + tid] = (csum[par][0][tid] + csum[par][1][tid]) + (csum[par][2][tid] + csum[par][3][tid]);
     };
@@ -403,14 +403,14 @@ key_weight_small_kernel(const Args a)
     __shared__ __attribute__((aligned(1024))) char rows[SNW * C::SUB];      // 32 of K a wave
     __shared__ __attribute__((aligned(1024))) char qrows[C::SUB];
     __shared__ __attribute__((aligned(16))) Taken prod[2][SNW][32];         // per round parity: a wave's keys
-    const int unit = a.groups - 1 - (int)blockIdx.x, bkv = blockIdx.y;
+    const int at = a.groups - 1 - (int)blockIdx.x, unit = a.first + at, bkv = blockIdx.y;
     const int b = bkv / a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, hh = lane >> 5;
     const int len = length_of(a.lens, b, a.T), qlen = length_of(a.qlens, b, a.Tq);
     const Unit u = unit_of(a, unit, bkv, len - qlen, qlen, n);
-    int* const reach = a.reach + ((long)bkv * a.groups + unit) * 2;
+    int* const reach = a.reach + ((long)bkv * a.groups + at) * 2;
     double stick = u.there ? 1.0 : 0.0;
     if (u.some == 0) {
         if (tid == 0) reach[0] = reach[1] = 0;
@@ -443,7 +443,7 @@ key_weight_small_kernel(const Args a)
     bf16x8 qf[1][D / 16];
     read_q<D>(qf[0], lds_offset(qrows), n, hh, u.there);
 
-    float* const part = a.part + ((long)bkv * a.groups + unit) * a.Tpad;
+    float* const part = a.part + ((long)bkv * a.groups + at) * a.Tpad;
     for (int par = 0; hi > 0; par ^= 1) {
         const int base = hi - 32 * (wave + 1);
         dma_wait<0>();
@@ -525,12 +525,23 @@ key_weight_sum_kernel(const Args a)
     }
 }
 
+// Numbers in the workspace at a time: 2 GiB (chunks of keys, 384 groups at most, take less).  B1 H32 Hkv8 T131072 d128 takes four times two launches, 10.3 ms
+// with a third of the kv heads far, 34.4 with all; with 8 GiB at once 9.7 and 33.4.
+constexpr long MOST_PART = 1L << 29;
+
 struct Plan {
     bool small, pairs;
     int groups, chunks, C;
     int Tpad;
-    int units() const { return small ? groups : groups * NW; }
-    size_t floats(int BHkv) const { return (size_t)BHkv * ((size_t)groups * (Tpad + 2 * (size_t)chunks) + (chunks > 1 ? (size_t)units() * chunks * 64 : 0)); }
+    // groups at a time: their numbers go through the workspace, which for all of them would grow with T^2
+    int at_once(int BHkv) const
+    {
+        const long most = chunks > 1 ? groups : std::max(1L, std::min<long>(groups, MOST_PART / ((long)BHkv * Tpad)));
+        const long times = (groups + most - 1) / most;
+        return (int)((groups + times - 1) / times);
+    }
+    size_t left_of() const { return chunks > 1 ? (size_t)groups * NW * chunks * 32 : 0; }
+    size_t floats(int BHkv) const { return (size_t)BHkv * ((size_t)at_once(BHkv) * (Tpad + 2 * (size_t)chunks) + 2 * left_of()); }
 };
 // What a plan takes, from measurements (all heads far; us).  One unit a workgroup: 1.25 for a round of 256 keys, of the longest unit alone where the
 // units fit the chip, 256 of them at a time beyond.  Four units: 1.4 for a tile of 64 keys of the longest, or 0.45 ns a subtile of all, whichever is more.  Chunks of
@@ -594,20 +605,25 @@ hipError_t launch_key_weight(const uint16_t* q, const uint16_t* k, const int* le
                              float* workspace, int B, int H, int Hkv, int Tq, int T, int Tcap, int d, hipStream_t stream)
 {
     const Plan p = plan_of(B, H, Hkv, Tq, T);
-    const int BHkv = B * Hkv;
-    Args a = {q, k, lens, qlens, score, score_out, workspace, nullptr, nullptr, H, Hkv, H / Hkv, Tq, T, Tcap, p.Tpad, p.groups, p.chunks, p.C};
-    a.left = reinterpret_cast<double*>(workspace + (size_t)BHkv * p.groups * p.Tpad);
-    a.reach = reinterpret_cast<int*>(a.left + (p.chunks > 1 ? (size_t)BHkv * p.units() * p.chunks * 32 : 0));
-    const hipError_t e = d == 32 ? launch_d<32>(a, p, BHkv, stream) : d == 64 ? launch_d<64>(a, p, BHkv, stream) : launch_d<128>(a, p, BHkv, stream);
-    if (e != hipSuccess) return e;
-    // no more waves than have a group to add (B4 H16 T8192 d64, 128 rows, 4 groups: 9 us in all with one wave, 15.5 with eight)
-    auto sum = [&](auto kernel, int waves) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((T + 63) / 64), (unsigned)BHkv), dim3(64 * waves), 0, stream, a);
-    };
-    if (p.groups <= SUM_DEEP) sum(key_weight_sum_kernel<1>, 1);
-    else if (p.groups <= 2 * SUM_DEEP) sum(key_weight_sum_kernel<2>, 2);
-    else sum(key_weight_sum_kernel<8>, 8);
-    return hipGetLastError();
+    const int BHkv = B * Hkv, most = p.at_once(BHkv);
+    Args a = {q, k, lens, qlens, score, score_out, workspace, nullptr, nullptr, H, Hkv, H / Hkv, Tq, T, Tcap, p.Tpad, most, p.chunks, p.C, 0};
+    a.left = reinterpret_cast<double*>(workspace + (size_t)BHkv * most * p.Tpad);
+    a.reach = reinterpret_cast<int*>(a.left + BHkv * p.left_of());
+    for (; a.first < p.groups; a.first += most) {
+        a.groups = std::min(most, p.groups - a.first);
+        hipError_t e = d == 32 ? launch_d<32>(a, p, BHkv, stream) : d == 64 ? launch_d<64>(a, p, BHkv, stream) : launch_d<128>(a, p, BHkv, stream);
+        if (e != hipSuccess) return e;
+        // no more waves than have a group to add (B4 H16 T8192 d64, 128 rows, 4 groups: 9 us in all with one wave, 15.5 with eight)
+        auto sum = [&](auto kernel, int waves) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((T + 63) / 64), (unsigned)BHkv), dim3(64 * waves), 0, stream, a);
+        };
+        if (a.groups <= SUM_DEEP) sum(key_weight_sum_kernel<1>, 1);
+        else if (a.groups <= 2 * SUM_DEEP) sum(key_weight_sum_kernel<2>, 2);
+        else sum(key_weight_sum_kernel<8>, 8);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        a.score = score_out;                               // the groups before
+    }
+    return hipSuccess;
 }
 
 }  // namespace sb

@@ -23,3 +23,10 @@ def test_decode_in_one_launch_needs_no_room_for_weights(lib):
     need = lib.sb_attn_decode_kv4_workspace_bytes
     for B, H, Hkv, T, d in ((32, 64, 64, 1000, 128), (32, 16, 16, 1800, 64), (1, 12, 4, 333, 128), (64, 64, 4, 700, 32)):
         assert need(B, H, Hkv, T, 65536, d, 1) == need(B, H, Hkv, T, 65536, d, 0) <= 4 * B * H * (d + 4)
+
+
+def test_key_weights_of_long_prompts_stay_within_two_gigabytes(lib):
+    """One number a key from each workgroup, 2^31 bytes of them at a time (or a workgroup a kv head), and two integers a workgroup."""
+    need = lib.sb_attn_key_weight_workspace_bytes
+    for B, H, Hkv, Tq, T in ((1, 32, 8, 131_072, 131_072), (1, 32, 8, 524_288, 524_288), (16, 32, 32, 65_536, 65_536), (1, 64, 64, 262_144, 524_288), (300, 3, 1, 1, 524_288)):
+        assert 0 < need(B, H, Hkv, Tq, T, 128) <= max(2 ** 31, 4 * T * B * Hkv) + 2 ** 20, (B, H, Hkv, Tq, T)
