@@ -250,8 +250,9 @@ int sb_attn_decode_static(const void* q, const void* k, const void* v, const voi
  *                      power of two, 2^-120 at least, of which no magnitude is more than 7 times;
  *                      values are rounded to the nearest, ties to the even code, beyond 6 to 6.  A
  *                      block that holds a NaN or an infinity gets E = 255 and is NaN throughout.
- *   sb_attn_kv4_load   the values of those rows as bf16 [B, Hkv, n, d], exactly; zeros for rows
- *                      outside the cache.
+ *                      (Finite magnitudes beyond 1.75 * 2^127 round to 4 * 2^126 or more: infinity in bf16.)
+ *   sb_attn_kv4_load   the values of those rows as bf16 [B, Hkv, n, d], exactly, infinity where they
+ *                      are 2^128 and more; zeros for rows outside the cache.
  */
 int sb_attn_kv4_store(const void* k, const void* v, void* kc, void* ks, void* vc, void* vs, const int* pos,
                       int B, int Hkv, int n, int Tcap, int d, void* stream);
