@@ -268,8 +268,9 @@ int sb_attn_kv4_load(const void* kc, const void* ks, const void* vc, const void*
  * heads of kv head h of A[i], for the entry's rows i; others are left as they were.  score may be
  * NULL (zeros) and may be score_out itself, but not overlap it otherwise (SB_ERR_OVERLAP).  At most
  * 1024 query heads a kv head and B*H <= 8388607 with score_out (16777215 without).
- * Weights have fp32's 24 bits, in o (which is rounded once, at its end) and in score.  Rows of
- * which less than 2^-126 of the stick is left count as zero, a NaN among them too, as long as m is not wanted.
+ * Weights have fp32's 24 bits, in o (which is rounded once, at its end) and in score.  Where less
+ * than 2^-126 of the stick is left a weight may be taken as zero and, as long as m is not wanted, its row left unread: a NaN or an
+ * infinity from there on may or may not reach o and score.
  * workspace: sb_attn_decode_kv4_workspace_bytes(B, H, Hkv, T, Tcap, d, score_out != NULL) bytes: 4*d + 12 a query head and
  * chunk (at most 128), and with scores 4*T a query head where it has more than one chunk or a kv head more than 16.
  * Bit-reproducible, as sb_attn_decode.
@@ -283,7 +284,8 @@ int sb_attn_decode_kv4(const void* q, const void* kc, const void* ks, const void
  * The weight that a prompt's queries give each key: score_out[b,h,i] = score[b,h,i] + sum over query
  * rows j and the query heads of kv head h of A[i,j] (Eq. 1), for the entry's rows i; others are left
  * as they were.  score may be NULL (zeros) and may be score_out itself, but not overlap it otherwise
- * (SB_ERR_OVERLAP).  Keys of which a query has less than 2^-126 of its stick left get nothing from it.
+ * (SB_ERR_OVERLAP).  Where a query has less than 2^-126 of its stick left its weights may be taken as zero:
+ * a NaN or an infinity in keys from there on may or may not reach the sums.
  * q: bf16 [B, H, Tq, d]; k: bf16 [B, Hkv, Tcap, d].  lens, qlens: B ints each on the DEVICE, the rows
  * and the query rows of every entry, or NULL: T, Tq (clamped to 0 .. T and 0 .. Tq; what lies behind
  * them is not looked at).  The queries are those of the entry's last rows: query row t < qlens[b]

@@ -1,4 +1,4 @@
-"""The ends of the 4-bit format's range."""
+"""The ends of the 4-bit format's range, and keys that no stick is left for."""
 import pytest
 import torch
 
@@ -38,3 +38,27 @@ def test_largest_magnitudes(sb):
     inf, unit = float("inf"), 2.0 ** 126
     assert torch.equal(k, v) and k[0, 0, :, :3].double().tolist() == [[3 * unit, -2 * unit, unit], [inf, -3 * unit, unit], [-inf, inf, 2 * unit]]
     assert not k[0, 0, :, 3:].any()
+
+
+# one launch (a few workgroups, and more than the chip holds), spread, three launches
+@pytest.mark.parametrize("want_m", [False, True])
+@pytest.mark.parametrize("B,H,Hkv,T", [(1, 4, 2, 300), (300, 4, 2, 300), (2, 4, 2, 2500), (40, 8, 4, 5000)])
+def test_finite_keys_behind_a_used_up_stick_change_nothing(sb, B, H, Hkv, T, want_m):
+    """The nearest 12 keys, logits of 40, leave 2^-690 of the stick: other rows behind them make no bit of o another one, m of its own keys apart, and get weights of 2^-126 at most."""
+    d = 64
+    q, k, v = forms.activations(B, H, Hkv, T, d, seed=B + T)
+    k[:, :, T - 12:] = 0.0
+    k[:, :, T - 12:, 0] = 4.0
+    q[..., 0] = 80.0
+    k[:, :, :T - 12, 0] = 0.0
+    got = []
+    for sign in (1.0, -2.0):
+        cache = forms.new_cache(B, Hkv, (T + 31) // 32 * 32, d)
+        other = torch.where(torch.arange(T, device="cuda")[:, None] < T - 12, sign, 1.0)
+        sb.sb_attn_kv4_store((k * other).bfloat16(), (v * other).bfloat16(), *cache)
+        got.append(sb.sb_attn_decode_kv4(q, *cache, T=T, score_out=torch.zeros(B, Hkv, cache[0].shape[2], device="cuda"), want_m=want_m))
+    (a, b) = got
+    assert torch.isfinite(a[0]).all() and torch.equal(a[0], b[0]) and torch.equal(a[-1][:, :, T - 12:], b[-1][:, :, T - 12:])
+    assert (a[-1][:, :, T - 1] > 0.99 * H // Hkv).all() and max(float(x[-1][:, :, :T - 12].max()) for x in got) <= (H // Hkv) * 2.0 ** -126
+    if want_m:
+        assert torch.isfinite(a[1]).all() and (a[1] < -470).all()
