@@ -24,8 +24,9 @@
 //            eight rows of V, converts, and an in-register transposition (one v_perm per packed pair) makes the A operands.
 // Codes and scales come through LDS as whole rows, every wave its own, one round ahead: K's place is asked for again as soon as a round
 // has its logits, V's behind its output.  (Straight to registers it is 14 loads a tile, and 26 registers a tile to hold them: all heads far, B8 H16 T16384, d = 128, 64, 32:
-// 69, 52, 37 us, through LDS with the same rounds 65, 44, 36.)  A near launch of more workgroups than the chip holds takes half as many waves a workgroup, two tiles each:
-// B32 H16 T2000 d128 9.8 -> 8.5 us with no head far, 30.5 -> 24.6 with a third; smaller ones lose by it (B16 H8 T2000 d128 15.2 -> 17.8).
+// 69, 52, 37 us, through LDS with the same rounds 65, 44, 36, both before what is said of small weights and parts here.)  A near launch of more workgroups than the chip holds takes half
+// as many waves a workgroup, two tiles each: B32 H16 T2000 d128 10.5 -> 8.9 us with no head far, 32.4 -> 21.3 with a third, B40 H16 T1800 d64 9.2 -> 7.7, 21.5 -> 18.1; smaller ones lose by it
+// (B16 H8 T2000 d128 5.5 -> 6.3, 16.9 -> 18.2, B32 H16 T1800 d64 6.9 -> 6.8, 16.5 -> 17.1).
 // V meets a weight in three parts of eight bits, bf16 each: 24 bits, all that it has, as in sb_decode.hip.  (Two parts, 16 bits, took 1 to 3 % less: B8 H16 T16384 d128, all far,
 // 55.5 / 55.9 us, B32 H16 T1800 d64 19.4 / 20.0.)
 // The 16 columns of the MFMAs are more than most groups have heads.  Their copies of a head take a tile each (two with up to four heads, R), which
@@ -69,8 +70,8 @@ __device__ __forceinline__ int length_of(const Args& a, int b)
 __device__ __forceinline__ int up32(int n) { return (n + 31) & ~31; }
 
 // The entry and kv head of a near workgroup.  A CU gets workgroups i, i + 256, ..: with 16 kv heads, the same head of several entries, and heads that reach far would come
-// together.  So the heads of an entry turn by one for each 256 workgroups in front of it (B32 H16 T1800 d64, a third of the heads far, 18.2 -> 15.4 us, d128 23.7 -> 20.5; none
-// far 6.7 -> 6.7, at d = 32 6.0 -> 6.4).
+// together.  So the heads of an entry turn by one for each 256 workgroups in front of it (B32 H16 T1800 d64, a third of the heads far, 20.6 -> 16.4 us, d128 25.2 -> 21.7,
+// d32 18.9 -> 15.4; none far 7.3 -> 7.3, 8.8 -> 9.0, 6.8 -> 6.8; all far 21.3 -> 21.9, 29.3 -> 30.1, 19.9 -> 19.9).
 __device__ __forceinline__ int turned(int wg, int Hkv)
 {
     const int first = wg / Hkv * Hkv;
@@ -662,7 +663,7 @@ decode_kv4_combine_kernel(const Args a, int H, int heads)
     }
 }
 
-// Workgroups of the near launch that one round of the chip holds: eight waves of 146 registers and 68 KB, 112 and 35 KB, 89 and 19 KB.
+// Workgroups of the near launch that one round of the chip holds: eight waves of 147 to 152 registers and 69 KB, 116 to 127 and 36 KB, 92 to 111 and 20 KB.
 constexpr long round_of(int d) { return d == 128 ? 256 : 512; }
 
 // the heads' weights meet in a launch of their own

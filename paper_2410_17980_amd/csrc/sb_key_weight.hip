@@ -546,11 +546,11 @@ struct Plan {
 // What a plan takes, from measurements (all heads far; us).  One unit a workgroup: 1.25 for a round of 256 keys, of the longest unit alone where the
 // units fit the chip, 256 of them at a time beyond.  Four units: 1.4 for a tile of 64 keys of the longest, or 0.45 ns a subtile of all, whichever is more.  Chunks of
 // keys in two launches: 8 more, 0.8 ns a subtile.  Measured with all heads far, one unit / four units / chunks (768 workgroups):
-//   B4 H12 Hkv4 T2048 d128, whole prompt 73 / 52;  B8 H16 T2048 d64 156 / 95;  B1 H12 Hkv4 T3000 d64 36 / 55 / 59;  B1 H4 T4000 d128 38 / 84 / 50;
-//   B2 H16 Hkv8 T700 d128 16.5 / 19 / 19;  64 rows of B1 H32 Hkv8 T16384 d128 - / 309 / 38;  one row of B1 H32 Hkv8 T4000 d128 27 / 80 / 16
+//   B4 H12 Hkv4 T2048 d128, whole prompt 78 / 56;  B8 H16 T2048 d64 173 / 101;  B1 H12 Hkv4 T3000 d64 39 / 56 / 70;  B1 H4 T4000 d128 40 / 85 / 54;
+//   B2 H16 Hkv8 T700 d128 16.5 / 19 / 20;  64 rows of B1 H32 Hkv8 T16384 d128 93 / 315 / 39;  one row of B1 H32 Hkv8 T4000 d128 27 / 82 / 16
 // Two units a wave where the longest workgroup's tiles, 2.1 each, take no longer than all the work does with a third of the kv heads far.  One / two, a third
-// far, then all:  B16 H16 T2048 d32 102 / 87, 173 / 138;  B2 H64 Hkv8 T4096 d64 139 / 133, 328 / 279;  B8 H32 Hkv8 T2048 d128 113 / 111, 231 / 211;
-//   B8 H16 T4096 d64 167 / 175, 347 / 302;  not B8 H16 T2048 d64 63 / 64, 98 / 86;  B1 H32 Hkv8 T8192 d128 199 / 264, 417 / 414
+// far, then all:  B16 H16 T2048 d32 109 / 97, 181 / 153;  B2 H64 Hkv8 T4096 d64 148 / 139, 339 / 287;  B8 H32 Hkv8 T2048 d128 108 / 114, 224 / 213;
+//   B8 H16 T4096 d64 174 / 174, 352 / 310;  not B8 H16 T2048 d64 66 / 66, 101 / 89;  B1 H32 Hkv8 T8192 d128 184 / 271, 409 / 412
 Plan plan_of(int B, int H, int Hkv, int Tq, int T)
 {
     const int G = H / Hkv, units = (Tq + 31) / 32 * G, Tpad = (T + TK - 1) / TK * TK;
